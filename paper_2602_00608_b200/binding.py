@@ -23,6 +23,10 @@ VD_FLAG_NO_CLUSTERS = 0x20
 VD_IMPL_AUTO, VD_IMPL_SIMT, VD_IMPL_TC, VD_IMPL_TC_SPLIT, VD_IMPL_TC_F32 = 0, 1, 2, 3, 4
 VD_ROUTE_DIRECT, VD_ROUTE_THIN, VD_ROUTE_F32, VD_ROUTE_TC, VD_ROUTE_SPLIT, VD_ROUTE_SPLIT_PAIRS, VD_ROUTE_F32_TC = 0, 1, 2, 3, 4, 5, 6
 VD_STEP_INGEST, VD_STEP_GN_STATS, VD_STEP_CONV, VD_STEP_ATTENTION = 0, 1, 2, 3
+VD_XATTN_AUTO, VD_XATTN_PLAIN = 0, 1
+VD_ROTARY_HALF, VD_ROTARY_INTERLEAVED, VD_ROTARY_MAX_AXES = 0, 1, 4
+VD_ROTARY_SCALE_NONE, VD_ROTARY_SCALE_LINEAR, VD_ROTARY_SCALE_BASE, VD_ROTARY_SCALE_PARTS = 0, 1, 2, 3
+VD_NORM_LAYER, VD_NORM_RMS = 0, 1
 STATUS_NAMES = {0: "VD_OK", -1: "VD_ERR_INVALID_ARG", -2: "VD_ERR_UNSUPPORTED", -3: "VD_ERR_WORKSPACE",
                 -4: "VD_ERR_CUDA", -5: "VD_ERR_DEVICE_TIMEOUT"}
 
@@ -31,6 +35,7 @@ EXPORTED = [
     "vd_last_error", "vd_destroy", "vd_num_steps", "vd_get_step", "vd_profile", "vd_debug_stop_after",
     "vd_conv_packed_weight_bytes", "vd_conv_pack_weight", "vd_op_conv2d", "vd_conv_route", "vd_op_conv2d_ex", "vd_conv_record_slots", "vd_op_merge_records", "vd_conv_stats_scratch_bytes", "vd_op_conv2d_stats", "vd_gn_scratch_bytes", "vd_op_gn_stats", "vd_op_gn_stats_single",
     "vd_op_attention", "vd_attention_scratch_bytes", "vd_op_gn_stats_static", "vd_clear_status", "vd_decode_host_stream", "vd_debug_check_canaries", "vd_debug_status_offset", "vd_debug_wait_probe",
+    "vd_op_cross_attention", "vd_op_rotary", "vd_rotary_frequencies", "vd_op_gate_norm",
 ]
 
 
@@ -66,6 +71,37 @@ class VdConvExtra(Structure):
                 ("in_records", c_void_p), ("in_gamma", c_void_p), ("in_beta", c_void_p), ("in_slots", c_int32),
                 ("in_groups", c_int32), ("in_eps", c_float), ("out_groups", c_int32), ("out_records", c_void_p),
                 ("out_pending", c_void_p)]
+
+
+class VdXattnDesc(Structure):
+    _fields_ = [("struct_size", c_uint32), ("dtype", c_int32), ("batch", c_int32), ("q_len", c_int32), ("kv_len", c_int32),
+                ("heads", c_int32), ("kv_heads", c_int32), ("head_dim", c_int32), ("impl", c_int32), ("scale", c_float),
+                ("q_batch", c_int64), ("q_token", c_int64), ("q_head", c_int64), ("k_batch", c_int64), ("k_token", c_int64),
+                ("k_head", c_int64), ("v_batch", c_int64), ("v_token", c_int64), ("v_head", c_int64), ("o_batch", c_int64),
+                ("o_token", c_int64), ("o_head", c_int64)]
+
+
+class VdRotaryDesc(Structure):
+    _fields_ = [("struct_size", c_uint32), ("dtype", c_int32), ("batch", c_int32), ("tokens", c_int32), ("heads", c_int32),
+                ("head_dim", c_int32), ("rotary_dim", c_int32), ("layout", c_int32), ("axes", c_int32),
+                ("axis_pairs", c_int32 * VD_ROTARY_MAX_AXES), ("amplitude", c_float), ("x_batch", c_int64), ("x_token", c_int64),
+                ("x_head", c_int64), ("y_batch", c_int64), ("y_token", c_int64), ("y_head", c_int64), ("pos_batch", c_int64),
+                ("pos_token", c_int64), ("first_position", c_int64)]
+
+
+class VdRotaryFreqDesc(Structure):
+    _fields_ = [("struct_size", c_uint32), ("rotary_dim", c_int32), ("axes", c_int32), ("axis_pairs", c_int32 * VD_ROTARY_MAX_AXES),
+                ("scaling", c_int32), ("base", c_double), ("factor", c_double), ("original_len", c_double), ("fast", c_double),
+                ("slow", c_double)]
+
+
+class VdGateNormDesc(Structure):
+    _fields_ = [("struct_size", c_uint32), ("batch", c_int32), ("tokens", c_int32), ("channels", c_int32), ("x_dtype", c_int32),
+                ("h_dtype", c_int32), ("y_dtype", c_int32), ("mod_dtype", c_int32), ("norm", c_int32), ("post_norm", c_int32),
+                ("mod_tokens", c_int32), ("eps", c_float), ("residual_scale", c_float), ("x_batch", c_int64), ("x_token", c_int64),
+                ("h_batch", c_int64), ("h_token", c_int64), ("xo_batch", c_int64), ("xo_token", c_int64), ("y_batch", c_int64),
+                ("y_token", c_int64), ("gate_batch", c_int64), ("gate_group", c_int64), ("scale_batch", c_int64),
+                ("scale_group", c_int64), ("shift_batch", c_int64), ("shift_group", c_int64)]
 
 
 class VdError(RuntimeError):
@@ -121,6 +157,10 @@ def lib():
         l.vd_op_attention.argtypes = [vp, vp, vp, vp, c_int32, c_int32, c_int32, c_int32, c_int32, c_int32, c_float, c_int32, vp, vp]
         l.vd_attention_scratch_bytes.argtypes = [c_int32, c_int32, c_int32]
         l.vd_attention_scratch_bytes.restype = c_size_t
+        l.vd_op_cross_attention.argtypes = [POINTER(VdXattnDesc), vp, vp, vp, vp, vp, vp]
+        l.vd_op_rotary.argtypes = [POINTER(VdRotaryDesc), vp, vp, vp, vp, vp]
+        l.vd_rotary_frequencies.argtypes = [POINTER(VdRotaryFreqDesc), POINTER(c_double)]
+        l.vd_op_gate_norm.argtypes = [POINTER(VdGateNormDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         for name in EXPORTED:
             if name not in ("vd_last_error", "vd_gn_scratch_bytes", "vd_attention_scratch_bytes"):
                 getattr(l, name).restype = c_int32
@@ -456,3 +496,176 @@ def op_attention(qkv, channels: int, scale: float, impl=VD_IMPL_AUTO):
                                  c_void_p(o.data_ptr()), _dt(qkv), b, t, channels, c3, channels, scale, impl,
                                  c_void_p(scratch.data_ptr()), _stream_ptr()))
     return o
+
+
+# ---- operators of a latent world model's transformer block (include/vd_block.h) -----------------
+def _refuse(msg: str):
+    raise VdError(VD_ERR_INVALID_ARG, msg)
+
+
+def _block_dtype(t, name: str) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return VD_BF16
+    if t.dtype != torch.float32:
+        _refuse(f"{name}: float32 or bfloat16, not {t.dtype}")
+    return VD_F32
+
+
+def _launch(device, call):
+    """call(stream) with the tensors' device current, on its current stream."""
+    import torch
+    if device.index == torch.cuda.current_device():
+        _check(call(torch.cuda.current_stream().cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(call(torch.cuda.current_stream().cuda_stream))
+
+
+def _on_device(ref, **others):
+    if not ref.is_cuda:
+        _refuse("tensors must be on a CUDA device")
+    for name, t in others.items():
+        if t is not None and t.device != ref.device:
+            _refuse(f"{name} is on {t.device}, not on {ref.device}")
+
+
+def op_cross_attention(q, k, v, kv_lens=None, scale=None, out=None, impl=VD_XATTN_AUTO):
+    """Attention of q [B,Tq,H,D] to k and v [B,Tk,Hkv,D] (H a multiple of Hkv; float32 or bfloat16; slices and expanded tensors
+    are taken as they are, channels side by side) -> [B,Tq,H,D].  kv_lens: int32 [B], the keys of each item, or None for
+    all Tk; a row without keys is zeros.  scale: D ** -0.5 if None.  Gradients are not taken."""
+    import torch
+    if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape:
+        _refuse("q [B,Tq,H,D], k and v [B,Tk,Hkv,D]")
+    b, tq, h, d = q.shape
+    kb, tk, hkv, kd = k.shape
+    if kb != b or kd != d:
+        _refuse("q, k and v disagree in batch or head size")
+    if out is None:
+        out = torch.empty((b, tq, h, d), dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape:
+        _refuse("out must have q's shape")
+    if not q.dtype == k.dtype == v.dtype == out.dtype:
+        _refuse("q, k, v and out must have one type")
+    _on_device(q, k=k, v=v, kv_lens=kv_lens, out=out)
+    if kv_lens is not None and (kv_lens.dtype != torch.int32 or kv_lens.shape != (b,) or not kv_lens.is_contiguous()):
+        _refuse("kv_lens must be a contiguous int32 tensor [B]")
+    sq, sk, sv, so = q.stride(), k.stride(), v.stride(), out.stride()
+    if d > 1 and not sq[3] == sk[3] == sv[3] == so[3] == 1:
+        _refuse("the channels of a head must lie side by side")
+    desc = VdXattnDesc(ctypes.sizeof(VdXattnDesc), _block_dtype(q, "q"), b, tq, tk, h, hkv, d, impl, d ** -0.5 if scale is None else scale,
+                       sq[0], sq[1], sq[2], sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], so[0], so[1], so[2])
+    lens = None if kv_lens is None else kv_lens.data_ptr()
+    _launch(q.device, lambda stream: lib().vd_op_cross_attention(byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), lens, out.data_ptr(), stream))
+    return out
+
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, *, axis_pairs=None, scaling=VD_ROTARY_SCALE_NONE, factor: float = 1.0,
+                       original_len: float = 0.0, fast: float = 32.0, slow: float = 1.0):
+    """The frequencies of op_rotary (float64 CPU tensor [rotary_dim / 2], turns per position): see vd_rotary_frequencies."""
+    import torch
+    pairs = [rotary_dim // 2] if axis_pairs is None else list(axis_pairs)
+    if len(pairs) > VD_ROTARY_MAX_AXES:
+        _refuse("too many axes")
+    desc = VdRotaryFreqDesc(ctypes.sizeof(VdRotaryFreqDesc), rotary_dim, len(pairs), (c_int32 * VD_ROTARY_MAX_AXES)(*pairs), scaling, base,
+                            factor, original_len, fast, slow)
+    out = (c_double * max(1, rotary_dim // 2))()
+    _check(lib().vd_rotary_frequencies(byref(desc), out))
+    return torch.tensor(out[:rotary_dim // 2], dtype=torch.float64)
+
+
+def op_rotary(x, freqs, positions=None, *, layout="half", axis_pairs=None, amplitude: float = 1.0, first_position: int = 0, out=None):
+    """Rotary positions of x [B,T,H,D] (float32 or bfloat16; q and k side by side in one tensor take one call): the first
+    2 * len(freqs) channels of each head turn, the others are copied.  freqs: float64 [R/2] on the device, turns per position
+    (rotary_frequencies).  positions: int32 [B,T] or [B,T,axes] (expanded over the batch is fine), or None: first_position, + 1, ...
+    axis_pairs: the pairs of each axis.  layout: "half" or "interleaved".  out may be x."""
+    import torch
+    if x.dim() != 4:
+        _refuse("x [B,T,H,D]")
+    b, t, h, d = x.shape
+    if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
+        _refuse("freqs must be a contiguous float64 tensor [R/2]")
+    n = freqs.shape[0]
+    pairs = (n,) if axis_pairs is None else tuple(axis_pairs)
+    if not 1 <= len(pairs) <= VD_ROTARY_MAX_AXES:
+        _refuse("bad number of axes")
+    if layout not in ("half", "interleaved"):
+        _refuse("layout: half or interleaved")
+    if out is None:
+        out = torch.empty((b, t, h, d), dtype=x.dtype, device=x.device)
+    elif out.shape != x.shape or out.dtype != x.dtype:
+        _refuse("out must have x's shape and type")
+    _on_device(x, freqs=freqs, positions=positions, out=out)
+    pb = pt = 0
+    if positions is not None:
+        if positions.dtype != torch.int32 or tuple(positions.shape) not in ((b, t, len(pairs)),) + (((b, t),) if len(pairs) == 1 else ()):
+            _refuse("positions must be int32 [B,T,axes]")
+        if len(pairs) > 1 and positions.stride(2) != 1:
+            _refuse("the axes of a position must lie side by side")
+        pb, pt = positions.stride(0), positions.stride(1)
+    sx, sy = x.stride(), out.stride()
+    if d > 1 and not sx[3] == sy[3] == 1:
+        _refuse("the channels of a head must lie side by side")
+    desc = VdRotaryDesc(ctypes.sizeof(VdRotaryDesc), _block_dtype(x, "x"), b, t, h, d, 2 * n, VD_ROTARY_INTERLEAVED if layout == "interleaved" else VD_ROTARY_HALF,
+                        len(pairs), (c_int32 * VD_ROTARY_MAX_AXES)(*pairs), amplitude, sx[0], sx[1], sx[2], sy[0], sy[1], sy[2], pb, pt,
+                        first_position)
+    at = None if positions is None else positions.data_ptr()
+    _launch(x.device, lambda stream: lib().vd_op_rotary(byref(desc), x.data_ptr(), at, freqs.data_ptr(), out.data_ptr(), stream))
+    return out
+
+
+def op_gate_norm(x, h=None, *, gate=None, scale=None, shift=None, kind="layer", eps: float = 1e-6, weight=None, bias=None, post_norm=False,
+                 post_weight=None, residual_scale: float = 1.0, mod_tokens=None, x_out=None, y=None, want_x=True, want_y=True):
+    """r = x + residual_scale * gate * u, u = h or norm(h) * post_weight, and y = (norm(r) * weight + bias) * (1 + scale) + shift, of tokens
+    [B,T,C] -> (r in x's type, y in h's type, or x's without h).  gate, scale, shift: [B,M,C] of one type, a row for every
+    mod_tokens tokens (M = ceil(T / mod_tokens); None: all of an item's).  weight, bias, post_weight: float32 [C].  kind: "layer" or
+    "rms".  x_out may be x, y may be h; want_x, want_y: False leaves that output out (None)."""
+    import torch
+    if x.dim() != 3 or (h is not None and h.shape != x.shape):
+        _refuse("x and h [B,T,C]")
+    b, t, c = x.shape
+    if kind not in ("layer", "rms"):
+        _refuse("kind: layer or rms")
+    mod_tokens = max(t, 1) if mod_tokens is None else mod_tokens
+    if mod_tokens < 1:
+        _refuse("mod_tokens must be positive")
+    x_out = (torch.empty((b, t, c), dtype=x.dtype, device=x.device) if x_out is None else x_out) if want_x else None
+    y = (torch.empty((b, t, c), dtype=x.dtype if h is None else h.dtype, device=x.device) if y is None else y) if want_y else None
+    for name, o in (("x_out", x_out), ("y", y)):
+        if o is not None and o.shape != x.shape:
+            _refuse(f"{name} must have x's shape")
+    if x_out is not None and x_out.dtype != x.dtype:
+        _refuse("x_out must have x's type")
+    groups, mod = -(-t // mod_tokens), None
+    strides = []
+    for name, m in (("gate", gate), ("scale", scale), ("shift", shift)):
+        if m is None:
+            strides += [0, 0]
+            continue
+        if m.shape != (b, groups, c) or (c > 1 and m.stride(2) != 1):
+            _refuse(f"{name} must be [B, {groups}, C], channels side by side")
+        if mod is not None and m.dtype != mod:
+            _refuse("gate, scale and shift must have one type")
+        mod = m.dtype
+        strides += [m.stride(0), m.stride(1)]
+    for name, w in (("weight", weight), ("bias", bias), ("post_weight", post_weight)):
+        if w is not None and (w.dtype != torch.float32 or w.shape != (c,) or not w.is_contiguous()):
+            _refuse(f"{name} must be a contiguous float32 tensor [C]")
+    _on_device(x, h=h, gate=gate, scale=scale, shift=shift, weight=weight, bias=bias, post_weight=post_weight, x_out=x_out, y=y)
+    rows = []
+    for name, r in (("x", x), ("h", h), ("x_out", x_out), ("y", y)):
+        if r is None:
+            rows += [0, 0]
+            continue
+        if c > 1 and r.stride(2) != 1:
+            _refuse(f"{name}: the channels of a token must lie side by side")
+        rows += [r.stride(0), r.stride(1)]
+    xd = _block_dtype(x, "x")
+    mods = next((m for m in (gate, scale, shift) if m is not None), None)
+    desc = VdGateNormDesc(ctypes.sizeof(VdGateNormDesc), b, t, c, xd, xd if h is None else _block_dtype(h, "h"), xd if y is None else _block_dtype(y, "y"),
+                          VD_F32 if mods is None else _block_dtype(mods, "gate, scale and shift"), VD_NORM_RMS if kind == "rms" else VD_NORM_LAYER,
+                          int(post_norm), mod_tokens, eps, residual_scale, *rows, *strides)
+    p = lambda v: None if v is None else v.data_ptr()
+    _launch(x.device, lambda stream: lib().vd_op_gate_norm(byref(desc), p(x), p(h), p(post_weight), p(gate), p(x_out), p(weight), p(bias),
+                                                           p(scale), p(shift), p(y), stream))
+    return x_out, y

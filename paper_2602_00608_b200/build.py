@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "build")
 LIB = os.path.join(PKG, "libvd.so")
-SOURCES = ["vd_api.cu", "kernels_simt.cu", "conv_tc.cu", "conv_split.cu", "conv_f32.cu", "conv_f32_tc.cu", "attn_tc.cu", "wait_probe.cu"]
+SOURCES = ["vd_api.cu", "kernels_simt.cu", "conv_tc.cu", "conv_split.cu", "conv_f32.cu", "conv_f32_tc.cu", "attn_tc.cu", "wait_probe.cu",
+           "block_api.cu", "xattn_plain.cu", "rotary.cu", "gate_norm.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC,-fvisibility=hidden", "-DVD_BUILD",
               "-I", os.path.join(ROOT, "include"), "-I", CSRC]
@@ -27,7 +28,7 @@ def _newer(target: str, deps) -> bool:
 def build(verbose: bool = False, force: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))]
-    headers += [os.path.join(ROOT, "include", f) for f in ("vd.h", "vd_ops.h")]
+    headers += [os.path.join(ROOT, "include", f) for f in ("vd.h", "vd_ops.h", "vd_block.h")]
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
     def compile_one(src: str) -> str:
