@@ -1,35 +1,121 @@
-// Rotary positions: one read and one write of the tensor.  angle = position * turns per position, in 64 bits: at position 10^6
-// an fp32 product would leave 2^-24 * 10^6 = 0.06 of a turn's last digits; the whole turns go before sin and cos are taken in fp32.
+// Rotary positions: one read and one write of the tensor.  angle = position * turns per position, in 64 bits: at position 10^6 an
+// fp32 product would leave 0.06 of a turn in doubt; the whole turns go before sin and cos are taken in fp32.
+// Bound by HBM.  A token's (cos, sin) are made once, in shared memory, and used by all its heads; a thread owns the same channels of
+// several heads, 16 bytes each, whose loads are under way while the table is made.
 #include "block_ops.h"
 
 namespace vd {
 namespace {
 
-__device__ __forceinline__ void sincos_of(const RotaryArgs& a, int b, int t, int pair, float* sn, float* cs) {
+__device__ __forceinline__ float2 turn_of(const RotaryArgs& a, int b, int t, int pair) {
     int axis = 0;
     while (axis < a.axes - 1 && pair >= a.axis_end[axis]) ++axis;
     const int64_t pos = a.pos ? (int64_t)a.pos[b * a.pos_batch + t * a.pos_token + axis] : a.first + t;
     const double turns = (double)pos * a.freqs[pair];
-    sincospif(2.f * (float)(turns - rint(turns)), sn, cs);
-    *sn *= a.amplitude;
-    *cs *= a.amplitude;
+    float sn, cs;
+    sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
+    return make_float2(cs * a.amplitude, sn * a.amplitude);
 }
 
-// a block per token; thread-strided over (head, pair or copied channel)
-__global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
-    extern __shared__ float2 turn[];                         // (cos, sin) of the token's pairs
+constexpr int MAX_THREADS = 256, HEADS = 4;                  // HEADS: of a thread, loaded ahead
+
+__device__ __forceinline__ void turn_pair(float& u, float& v, float2 cs) {
+    const float x = u;
+    u = fmaf(x, cs.x, -v * cs.y);
+    v = fmaf(x, cs.y, v * cs.x);
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&t);
+}
+// 16 bytes as V = 8 bf16 or 4 fp32 values
+__device__ __forceinline__ void up(const uint4& r, float (&f)[8]) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void up(const uint4& r, float (&f)[4]) {
+    f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
+}
+__device__ __forceinline__ uint4 down(const float (&f)[8]) { return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])); }
+__device__ __forceinline__ uint4 down(const float (&f)[4]) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+
+// blockDim: (units of a head, heads, tokens).  A unit is 16 bytes (HALF: of either half of the turned channels), or 16 copied bytes.
+template <typename T, bool HALF>
+__global__ void __launch_bounds__(MAX_THREADS) rotary_vec_kernel(const RotaryArgs a) {
+    constexpr int V = 16 / sizeof(T);
+    extern __shared__ float2 table[];                        // [tokens][pairs]
+    const int pairs = a.R / 2, turning = HALF ? pairs / V : a.R / V, unit = threadIdx.x;
+    const int64_t token = (int64_t)blockIdx.x * blockDim.z + threadIdx.z, tokens = (int64_t)a.B * a.T;
+    const bool here = token < tokens, turns = unit < turning;
+    const int b = here ? (int)(token / a.T) : 0, t = here ? (int)(token % a.T) : 0;
+    const int c = turns ? unit * V : a.R + (unit - turning) * V;
+    const T* x = (const T*)a.x + b * a.sx.batch + t * a.sx.token + c;
+    T* y = (T*)a.y + b * a.sy.batch + t * a.sy.token + c;
+    float2 cs[HALF ? V : V / 2];
+    for (int h0 = threadIdx.y; h0 < a.H; h0 += HEADS * (int)blockDim.y) {
+        uint4 r0[HEADS], r1[HEADS];
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) {
+            const int h = h0 + i * (int)blockDim.y;
+            if (here && h < a.H) {
+                r0[i] = *(const uint4*)(x + h * a.sx.head);
+                if (HALF && turns) r1[i] = *(const uint4*)(x + h * a.sx.head + pairs);
+            }
+        }
+        if (h0 == (int)threadIdx.y) {                        // (every thread has a head: blockDim.y <= H)
+            const int n = (int)(blockDim.x * blockDim.y * blockDim.z);
+            for (int i = ((int)threadIdx.z * blockDim.y + threadIdx.y) * blockDim.x + threadIdx.x; i < (int)blockDim.z * pairs; i += n) {
+                const int z = blockDim.z == 1 ? 0 : i / pairs;
+                const int64_t tk = (int64_t)blockIdx.x * blockDim.z + z;
+                if (tk < tokens) table[i] = turn_of(a, (int)(tk / a.T), (int)(tk % a.T), i - z * pairs);
+            }
+            __syncthreads();
+            if (turns)
+#pragma unroll
+                for (int e = 0; e < (HALF ? V : V / 2); ++e) cs[e] = table[threadIdx.z * pairs + (HALF ? unit * V : unit * V / 2) + e];
+        }
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) {
+            const int h = h0 + i * (int)blockDim.y;
+            if (!here || h >= a.H) continue;
+            if (turns) {
+                float f[V];
+                up(r0[i], f);
+                if (HALF) {
+                    float g[V];
+                    up(r1[i], g);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) turn_pair(f[e], g[e], cs[HALF ? e : 0]);
+                    *(uint4*)(y + h * a.sy.head + pairs) = down(g);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V / 2; ++e) turn_pair(f[2 * e], f[2 * e + 1], cs[e]);
+                }
+                r0[i] = down(f);
+            }
+            *(uint4*)(y + h * a.sy.head) = r0[i];
+        }
+    }
+}
+
+// any size and alignment: a block per token; thread-strided over (head, pair or copied channel)
+__global__ void __launch_bounds__(MAX_THREADS) rotary_kernel(const RotaryArgs a) {
+    extern __shared__ float2 table[];                        // of the token's pairs
     const int b = (int)(blockIdx.x / a.T), t = (int)(blockIdx.x % a.T), pairs = a.R / 2, work = pairs + a.D - a.R;
-    for (int i = threadIdx.x; i < pairs; i += blockDim.x) sincos_of(a, b, t, i, &turn[i].y, &turn[i].x);
+    for (int i = threadIdx.x; i < pairs; i += blockDim.x) table[i] = turn_of(a, b, t, i);
     __syncthreads();
     for (int64_t i = threadIdx.x; i < (int64_t)a.H * work; i += blockDim.x) {
         const int h = (int)(i / work), w = (int)(i % work);
         const int64_t x0 = b * a.sx.batch + t * a.sx.token + h * a.sx.head, y0 = b * a.sy.batch + t * a.sy.token + h * a.sy.head;
         if (w < pairs) {
             const int c0 = a.interleaved ? 2 * w : w, c1 = a.interleaved ? 2 * w + 1 : w + pairs;
-            const float u = load_as_f32(a.x, a.dtype, x0 + c0), v = load_as_f32(a.x, a.dtype, x0 + c1);
-            const float2 cs = turn[w];
-            store_from_f32(a.y, a.dtype, y0 + c0, fmaf(u, cs.x, -v * cs.y));
-            store_from_f32(a.y, a.dtype, y0 + c1, fmaf(u, cs.y, v * cs.x));
+            float u = load_as_f32(a.x, a.dtype, x0 + c0), v = load_as_f32(a.x, a.dtype, x0 + c1);
+            turn_pair(u, v, table[w]);
+            store_from_f32(a.y, a.dtype, y0 + c0, u);
+            store_from_f32(a.y, a.dtype, y0 + c1, v);
         } else {
             const int c = a.R + w - pairs;
             store_from_f32(a.y, a.dtype, y0 + c, load_as_f32(a.x, a.dtype, x0 + c));
@@ -37,10 +123,31 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
     }
 }
 
+template <typename T> cudaError_t launch_vec(const RotaryArgs& a, cudaStream_t s) {
+    constexpr int V = 16 / sizeof(T);
+    const int units = (a.interleaved ? a.R / V : a.R / 2 / V) + (a.D - a.R) / V;
+    const int heads = a.H < MAX_THREADS / units ? a.H : MAX_THREADS / units;
+    const int64_t tokens = (int64_t)a.B * a.T;
+    int per = MAX_THREADS / (units * heads);                 // small tokens share a block, as long as the blocks cover the GPU
+    while (per > 1 && (tokens + per - 1) / per < 4 * 148) --per;
+    if (per > 16) per = 16;
+    const dim3 grid((unsigned)((tokens + per - 1) / per)), block(units, heads, per);
+    const size_t smem = (size_t)per * (a.R / 2) * sizeof(float2);
+    if (a.interleaved) rotary_vec_kernel<T, false><<<grid, block, smem, s>>>(a);
+    else rotary_vec_kernel<T, true><<<grid, block, smem, s>>>(a);
+    return cudaGetLastError();
+}
+
 }  // namespace
 
 cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t s) {
-    rotary_kernel<<<(unsigned)(a.B * a.T), 256, a.R / 2 * sizeof(float2), s>>>(a);
+    const int size = a.dtype == VD_BF16 ? 2 : 4, V = 16 / size;
+    const uint64_t at = (uintptr_t)a.x | (uintptr_t)a.y |
+                        (uint64_t)((a.sx.batch | a.sx.token | a.sx.head | a.sy.batch | a.sy.token | a.sy.head) * size);
+    // 16 bytes at a time where every unit starts on such a boundary
+    if (at % 16 == 0 && a.D % V == 0 && a.R % (a.interleaved ? V : 2 * V) == 0)
+        return a.dtype == VD_BF16 ? launch_vec<__nv_bfloat16>(a, s) : launch_vec<float>(a, s);
+    rotary_kernel<<<(unsigned)((int64_t)a.B * a.T), MAX_THREADS, a.R / 2 * sizeof(float2), s>>>(a);
     return cudaGetLastError();
 }
 
