@@ -1,0 +1,478 @@
+// Attention to states of another length on tcgen05/TMEM (bf16, heads of up to 128 channels):
+//   o[b,t,h] = sum_{u < len[b]} softmax_u(scale q[b,t,h].k[b,u,h/g]) v[b,u,h/g]
+// An item is up to 256 rows of one key head: two tiles of 128 rows (a row is a token and one of the g heads that share the key head,
+// packed by the tensor map), each with a warpgroup of its own, one thread per row, so that a row's maximum and sum need no other
+// thread.  The two tiles take every block of 128 keys from shared memory together, and while one is in its softmax the tensor core
+// works for the other:
+//   S = Q K^T      K as it lies in memory, K-major
+//   softmax        running maximum with lazy rescaling of the output accumulator; exponentials partly on the FMA pipes (the special
+//                  function unit makes 16 a clock, 128 keys x 256 rows of them take as long as the products of 128 channels);
+//                  P in bf16 back to tensor memory, over S
+//   O += P V       P from tensor memory, V as it lies in memory (MN-major): nothing is transposed
+// CTAs are persistent, one per SM; the next item's Q, K and scores are under way during an item's last rows.
+// Keys behind a row's length: scores are replaced before the maximum, P is zero there, and the up to 15 rows of V that the last
+// product still reads are zeroed in shared memory, since 0 * NaN is NaN.
+// Every wait is bounded (see tc_common.cuh); rows of an item whose wait gave up are NaN.
+#include <algorithm>
+
+#include "block_ops.h"
+#include "conv_cluster.cuh"
+#include "tc_common.cuh"
+
+namespace vd {
+namespace {
+
+using namespace tc;
+
+constexpr int ROWS = 128, KEYS = 128, CHUNK = 64;            // of a tile; channels of a 128-byte row
+constexpr int SOFTMAX_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, NUM_THREADS = 320;
+constexpr float RESCALE_THRESHOLD = 8.0f;                    // log2 units: accumulators may grow by 2^8
+
+template <int DP> struct Cfg {
+    static constexpr int CHUNKS = DP / CHUNK;
+    static constexpr int TILE_BYTES = ROWS * DP * 2;         // of Q (a tile), K or V
+    static constexpr int STAGES = DP == 128 ? 3 : 6, Q_BUFS = 2;
+    static constexpr int SMEM = (Q_BUFS * 2 + STAGES) * TILE_BYTES + 512 + 1024;
+};
+struct Bars {
+    uint64_t q_full[2], q_empty[2], full[6], empty[6], s_full[2], p_full[2], o_full[2], drained;
+    uint32_t tmem_base, abort_flag;
+};
+static_assert(sizeof(Bars) <= 512 && Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448, "shared memory of one CTA");
+
+struct Params {
+    void* o;
+    const int32_t* lens;
+    int Tq, Tk, Hkv, g, D, nt;       // nt: tokens of a tile
+    int q_items;                     // items of a (batch item, key head)
+    int kb, vb, kh, vh;              // 0: the batch (head) coordinate of k or v stays 0
+    int64_t items, o_batch, o_token, o_head;
+    float scale_log2;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {       // NaN if one is
+    float y;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+__device__ __forceinline__ void unpack2(unsigned long long v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+// 2^x for a pair of x <= 8 on the FMA pipes: x = n + f, |f| <= 1/2, a polynomial of degree 4 for 2^f (coefficients fitted here to the
+// least largest relative error, 2^-18.5), n added to the exponent.  Below 2^-126 the result stays there.
+__device__ __forceinline__ void ex2_poly2(float& x, float& y) {
+    const unsigned long long v = pack2(fmaxf(x, -126.f), fmaxf(y, -126.f));
+    const unsigned long long t = add2(v, pack2(12582912.f, 12582912.f));             // 1.5 * 2^23: the sum's low bits are n
+    const unsigned long long f = fmaf2(add2(t, pack2(-12582912.f, -12582912.f)), pack2(-1.f, -1.f), v);
+    unsigned long long p = fmaf2(f, pack2(0.009570102f, 0.009570102f), pack2(0.055917859f, 0.055917859f));
+    p = fmaf2(p, f, pack2(0.24024744f, 0.24024744f));
+    p = fmaf2(p, f, pack2(0.69312179f, 0.69312179f));
+    p = fmaf2(p, f, pack2(0.99999928f, 0.99999928f));
+    float a, b, tx, ty;
+    unpack2(p, a, b);
+    unpack2(t, tx, ty);
+    x = __uint_as_float(__float_as_uint(a) + (__float_as_uint(tx) << 23));
+    y = __uint_as_float(__float_as_uint(b) + (__float_as_uint(ty) << 23));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const void* tmap, int c0, int c1, int c2, int c3, int c4, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+        ::"r"(dst), "l"(tmap), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(bar) : "memory");
+}
+// A from tensor memory, predicated like umma_bf16_split_on
+__device__ __forceinline__ void umma_bf16_ts_on(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                                uint32_t accumulate, uint32_t on) {
+    asm volatile(
+        "{\n.reg .pred p, q;\n.reg .b64 db;\nsetp.ne.b32 p, %5, 0;\nsetp.ne.b32 q, %6, 0;\nmov.b64 db, {%2, %3};\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n}\n"
+        ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(on) : "memory");
+}
+
+struct Item { int b, kvh, t0, streams, len, tiles; };
+__device__ __forceinline__ Item item_of(const Params& a, int64_t i) {
+    Item r;
+    const int qt = (int)(i % a.q_items), bh = (int)(i / a.q_items);
+    r.b = bh / a.Hkv;
+    r.kvh = bh - r.b * a.Hkv;
+    r.t0 = qt * 2 * a.nt;
+    r.streams = r.t0 + a.nt < a.Tq ? 2 : 1;
+    r.len = a.lens ? min(max(a.lens[r.b], 0), a.Tk) : a.Tk;
+    r.tiles = (r.len + KEYS - 1) / KEYS;
+    return r;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(NUM_THREADS, 1)
+xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                const __grid_constant__ CUtensorMap tm_v) {
+    using C = Cfg<DP>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem_q = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* smem_st = smem_q + C::Q_BUFS * 2 * C::TILE_BYTES;
+    Bars* bars = (Bars*)(smem_st + C::STAGES * C::TILE_BYTES);
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&bars->q_full[i]), 1); mbar_init(smem_u32(&bars->q_empty[i]), 1);
+            mbar_init(smem_u32(&bars->s_full[i]), 1); mbar_init(smem_u32(&bars->p_full[i]), SOFTMAX_WARPS / 2); mbar_init(smem_u32(&bars->o_full[i]), 1);
+        }
+        for (int i = 0; i < C::STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), 1); }
+        mbar_init(smem_u32(&bars->drained), 1);
+        bars->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async_smem();
+    }
+    if (warp == MMA_WARP) tmem_alloc(smem_u32(&bars->tmem_base), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem_base;                   // S (and P) of tile s at 128 s, O at 256 + DP s
+
+    if (warp < SOFTMAX_WARPS) {
+        // ------------------------------------------------------------ softmax: a thread per row
+        const int s = warp >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lanes + (uint32_t)s * 128u, t_o = tmem + lanes + 256u + (uint32_t)(s * DP);
+        const int tt = row / a.g, hg = row - tt * a.g;       // (once: a tile's packing is the same everywhere)
+        uint32_t n_s = 0, n_o = 0;                           // tiles and items so far
+        bool ok = true;
+        for (int64_t i = blockIdx.x; i < a.items; i += gridDim.x) {
+            const Item it = item_of(a, i);
+            if (s >= it.streams) continue;
+            float m_ref = -INFINITY;
+            unsigned long long l2 = 0, l2b = 0;
+            float l = 0.f;
+            for (int j = 0; j < it.tiles; ++j, ++n_s) {
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->s_full[s]), n_s & 1, abort_flag)) && ok;
+                tc_fence_after();
+                const int valid = it.len - j * KEYS;
+                uint32_t r[4][32];
+                float tmax;
+                if (valid >= KEYS) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld32(t_s + (uint32_t)c * 32u, r[c]);
+                    tmem_ld_wait();
+                    float m[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        m[c] = max3(__uint_as_float(r[c][0]), __uint_as_float(r[c][1]), __uint_as_float(r[c][2]));
+#pragma unroll
+                        for (int q = 3; q < 31; q += 2) m[c] = max3(m[c], __uint_as_float(r[c][q]), __uint_as_float(r[c][q + 1]));
+                        m[c] = max3(m[c], __uint_as_float(r[c][31]), __uint_as_float(r[c][31]));
+                    }
+                    tmax = max3(max3(m[0], m[1], m[2]), m[3], m[3]);
+                } else {                                     // keys that do not count leave before the maximum
+                    tmax = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if (c * 32 >= valid) break;
+                        tmem_ld32(t_s + (uint32_t)c * 32u, r[c]);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int q = 0; q < 32; ++q) {
+                            if (c * 32 + q >= valid) r[c][q] = __float_as_uint(-INFINITY);
+                            tmax = max3(tmax, __uint_as_float(r[c][q]), __uint_as_float(r[c][q]));
+                        }
+                    }
+                }
+                tmax *= a.scale_log2;
+                // lazy rescale: keep the old reference unless the maximum grew by more than the threshold
+                const bool grow = tmax > m_ref + RESCALE_THRESHOLD;
+                if (__any_sync(0xffffffffu, grow)) {
+                    float factor = 1.f;
+                    if (grow) {
+                        factor = ex2(m_ref - tmax);          // 0 at the first tile
+                        m_ref = tmax;
+                    }
+                    l *= factor;
+                    l2 = fmaf2(l2, pack2(factor, factor), 0ull);
+                    l2b = fmaf2(l2b, pack2(factor, factor), 0ull);
+                    if (j > 0) {                             // (the scores were issued behind the last product into O: it is complete)
+#pragma unroll 1
+                        for (uint32_t c = 0; c < (uint32_t)DP; c += 16u) {
+                            uint32_t o[16];
+                            tmem_ld16(t_o + c, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int q = 0; q < 16; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * factor);
+                            tmem_st16(t_o + c, o);
+                        }
+                    }
+                }
+                const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+                const unsigned long long sc = pack2(a.scale_log2, a.scale_log2), mr = pack2(-ref, -ref);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if (c * 32 >= valid) break;
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int q = 0; q < 32; q += 2) {
+                        float e0, e1;
+                        unpack2(fmaf2(pack2(__uint_as_float(r[c][q]), __uint_as_float(r[c][q + 1])), sc, mr), e0, e1);
+                        if ((q & 7) == 6 && valid >= KEYS) {         // a quarter
+                            ex2_poly2(e0, e1);
+                        } else {
+                            e0 = ex2(e0);
+                            e1 = ex2(e1);
+                        }
+                        if (q & 2) l2b = add2(l2b, pack2(e0, e1));
+                        else l2 = add2(l2, pack2(e0, e1));
+                        pk[q >> 1] = pack_bf16(e0, e1);
+                    }
+                    tmem_st16(t_s + (uint32_t)c * 16u, pk);
+                }
+                if (!(tmax < INFINITY)) l = __int_as_float(0x7fffffff);      // a NaN or an infinity among the scores
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars->p_full[s]));
+            }
+            if (it.tiles) {
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->o_full[s]), n_o & 1, abort_flag)) && ok;
+                tc_fence_after();
+                ++n_o;
+            }
+            l += sum2(add2(l2, l2b));
+            const float inv = it.tiles == 0 ? 0.f : ok ? 1.f / l : __int_as_float(0x7fffffff);
+            const int t = it.t0 + s * a.nt + tt;
+            const bool inside = tt < a.nt && t < a.Tq;
+            __nv_bfloat16* o = (__nv_bfloat16*)a.o + it.b * a.o_batch + t * a.o_token + (it.kvh * a.g + hg) * a.o_head;
+#pragma unroll
+            for (int c = 0; c < DP; c += 32) {
+                if (c >= a.D) break;
+                uint32_t v[32];
+                if (it.tiles) {
+                    tmem_ld32(t_o + (uint32_t)c, v);
+                    tmem_ld_wait();
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) v[q] = 0u;
+                }
+                if (inside)
+#pragma unroll
+                    for (int q = 0; q < 32; q += 8) {
+                        if (c + q >= a.D) break;
+                        float f[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(v[q + e]) * inv;
+                        *(uint4*)(o + c + q) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+                    }
+            }
+            tc_fence_before();                               // (the next product into O waits for this warp's next P)
+        }
+    } else if (warp == LOAD_WARP) {
+        // ------------------------------------------------------------ loads: Q, then K and V of each tile in turn
+        if (lane == 0) {
+            uint32_t st = 0, ph = 0;
+            int issued = 0, q_issued = 0;
+            bool ok = true;
+            for (int64_t i = blockIdx.x; i < a.items && ok; i += gridDim.x) {
+                const Item it = item_of(a, i);
+                if (!it.tiles) continue;
+                const int buf = q_issued & 1;
+                ok = mbar_wait(smem_u32(&bars->q_empty[buf]), ((q_issued >> 1) & 1) ^ 1, abort_flag);
+                if (!ok) break;
+                const uint32_t qf = smem_u32(&bars->q_full[buf]);
+                mbar_arrive_expect_tx(qf, (uint32_t)(it.streams * C::CHUNKS * a.g * a.nt * 128));
+                for (int s = 0; s < it.streams; ++s)
+                    for (int c = 0; c < C::CHUNKS; ++c)
+                        tma_load_5d(smem_u32(smem_q + (buf * 2 + s) * C::TILE_BYTES + c * (ROWS * 128)), &tm_q, c * CHUNK, 0, it.t0 + s * a.nt, it.kvh, it.b, qf);
+                ++q_issued;
+                for (int j = 0; j < 2 * it.tiles && ok; ++j) {
+                    ok = mbar_wait(smem_u32(&bars->empty[st]), ph ^ 1, abort_flag);
+                    if (!ok) break;
+                    const uint32_t full = smem_u32(&bars->full[st]);
+                    mbar_arrive_expect_tx(full, C::TILE_BYTES);
+                    for (int c = 0; c < C::CHUNKS; ++c) {
+                        const uint32_t dst = smem_u32(smem_st + st * C::TILE_BYTES + c * (KEYS * 128));
+                        if (j & 1) tma_load_4d(dst, &tm_v, c * CHUNK, (j >> 1) * KEYS, it.kvh * a.vh, it.b * a.vb, full);
+                        else tma_load_4d(dst, &tm_k, c * CHUNK, (j >> 1) * KEYS, it.kvh * a.kh, it.b * a.kb, full);
+                    }
+                    ++issued;
+                    if (++st == C::STAGES) { st = 0; ph ^= 1; }
+                }
+            }
+            // Everything has landed once it has been multiplied; if a wait gave up anywhere, before the CTA's memory goes.
+            for (int k = 0; k < C::STAGES && ok; ++k) {
+                ok = mbar_wait(smem_u32(&bars->empty[st]), ph ^ 1, abort_flag);
+                if (ok && ++st == C::STAGES) { st = 0; ph ^= 1; }
+            }
+            if (!ok) {
+                cc::land_loads(bars->q_full, 2, q_issued);
+                cc::land_loads(bars->full, C::STAGES, issued);
+            }
+        }
+    } else {
+        // ------------------------------------------------------------ MMA issue: the whole warp, instructions predicated on one lane
+        const uint32_t on = elect_one();
+        const uint32_t n_pv = (uint32_t)((a.D + 15) & ~15);
+        const uint32_t idesc_qk = make_idesc_bf16(128, KEYS), idesc_pv = make_idesc_bf16(128, n_pv) | (1u << 16);      // (bit 16: B is MN-major)
+        const uint32_t hi = desc_hi(1024, 2);
+        const int ksteps = (int)(n_pv >> 4);                 // of Q K^T
+        uint32_t st = 0, ph = 0, n_p[2] = {0, 0}, n_q = 0;
+        auto wait_on = [&](uint64_t* bar, uint32_t parity) {
+            const uint32_t p = smem_u32(bar);
+            if (!mbar_try_wait(p, parity)) (void)mbar_wait(p, parity, abort_flag);
+            tc_fence_after();
+        };
+        auto commit = [&](uint64_t* bar) { umma_commit_on(smem_u32(bar), on); };
+        auto step = [&]() { if (++st == C::STAGES) { st = 0; ph ^= 1; } };
+        auto issue_qk = [&](int s, uint32_t stage) {
+            const uint32_t q_lo = desc_lo(smem_u32(smem_q + ((n_q & 1) * 2 + s) * C::TILE_BYTES)), k_lo = desc_lo(smem_u32(smem_st + stage * C::TILE_BYTES));
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k) {
+                if (k >= ksteps) break;
+                const uint32_t at = (uint32_t)((k >> 2) * (ROWS * 128 >> 4) + (k & 3) * 2);
+                umma_bf16_split_on(tmem + (uint32_t)s * 128u, q_lo + at, hi, k_lo + at, hi, idesc_qk, k ? 1u : 0u, on);
+            }
+            commit(&bars->s_full[s]);
+            __syncwarp();
+        };
+        auto issue_pv = [&](int s, uint32_t stage, int steps, bool first) {
+            const uint32_t v_lo = desc_lo(smem_u32(smem_st + stage * C::TILE_BYTES)) | (((KEYS * 128u) >> 4) << 16);
+            const uint32_t d = tmem + 256u + (uint32_t)(s * DP), p = tmem + (uint32_t)s * 128u;
+#pragma unroll
+            for (int k = 0; k < KEYS / 16; ++k) {
+                if (k >= steps) break;
+                umma_bf16_ts_on(d, p + (uint32_t)k * 8u, v_lo + (uint32_t)k * (2048u >> 4), hi, idesc_pv, first && k == 0 ? 0u : 1u, on);
+            }
+            __syncwarp();
+        };
+        for (int64_t i = blockIdx.x; i < a.items; i += gridDim.x) {
+            const Item it = item_of(a, i);
+            if (!it.tiles) continue;
+            if (*abort_flag) break;
+            wait_on(&bars->q_full[n_q & 1], (n_q >> 1) & 1);
+            wait_on(&bars->full[st], ph);
+            for (int s = 0; s < it.streams; ++s) issue_qk(s, st);
+            commit(&bars->empty[st]);
+            if (it.tiles == 1) commit(&bars->q_empty[n_q & 1]);
+            step();
+            for (int j = 0; j < it.tiles; ++j) {
+                const uint32_t v_st = st;
+                const int valid = min(KEYS, it.len - j * KEYS), steps = (valid + 15) >> 4;
+                const bool last = j + 1 == it.tiles;
+                wait_on(&bars->full[st], ph);
+                step();
+                if (valid & 15) {                            // rows of V that count for nothing but are read
+                    for (int c = lane; c < (steps * 16 - valid) * 8; c += 32)
+#pragma unroll
+                        for (int x = 0; x < C::CHUNKS; ++x)
+                            *(uint4*)(smem_st + v_st * C::TILE_BYTES + x * (KEYS * 128) + valid * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                }
+                for (int s = 0; s < it.streams; ++s) {
+                    wait_on(&bars->p_full[s], n_p[s] & 1);
+                    ++n_p[s];
+                    issue_pv(s, v_st, steps, j == 0);
+                    if (s + 1 == it.streams) commit(&bars->empty[v_st]);
+                    if (last) {
+                        commit(&bars->o_full[s]);
+                    } else {
+                        if (s == 0) wait_on(&bars->full[st], ph);
+                        issue_qk(s, st);
+                        if (s + 1 == it.streams) {
+                            commit(&bars->empty[st]);
+                            if (j + 2 == it.tiles) commit(&bars->q_empty[n_q & 1]);
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (!last) step();
+            }
+            ++n_q;
+        }
+        if (*abort_flag) {                                   // nobody else waits for the products under way
+            commit(&bars->drained);
+            __syncwarp();
+            (void)cc::wait_cluster(smem_u32(&bars->drained), 0, abort_flag);
+            __syncwarp();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == MMA_WARP) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+bool encode(CUtensorMap* tm, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes, const uint32_t* box) {
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return false;
+    cuuint64_t d[5], st[4];
+    cuuint32_t bx[5], es[5];
+    for (int i = 0; i < rank; ++i) { d[i] = dims[i]; bx[i] = box[i]; es[i] = 1; }
+    for (int i = 0; i + 1 < rank; ++i) st[i] = strides_bytes[i];
+    return enc(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, st, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// bytes between the elements of a dimension; one that is never stepped along gets any valid stride
+bool stride_ok(int64_t stride, int64_t n, uint64_t* bytes) {
+    if (n <= 1) { *bytes = 256; return true; }
+    *bytes = (uint64_t)stride * 2;
+    return stride > 0 && stride % 8 == 0 && stride < (1ll << 38);
+}
+// k or v as [D, keys, heads, batch]; where a stride is 0 the coordinate stays 0
+bool encode_kv(CUtensorMap* tm, const XAttnArgs& a, const void* p, const Strides& s, int* use_head, int* use_batch) {
+    *use_head = s.head != 0;
+    *use_batch = s.batch != 0;
+    const uint64_t dims[4] = {(uint64_t)a.D, (uint64_t)a.Tk, s.head ? (uint64_t)a.Hkv : 1, s.batch ? (uint64_t)a.B : 1};
+    uint64_t st[3];
+    const uint32_t box[4] = {CHUNK, KEYS, 1, 1};
+    return stride_ok(s.token, dims[1], &st[0]) && stride_ok(s.head, dims[2], &st[1]) && stride_ok(s.batch, dims[3], &st[2]) && encode(tm, p, 4, dims, st, box);
+}
+
+template <int DP> cudaError_t launch(const Params& p, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, int sms, cudaStream_t s) {
+    const cudaError_t e = cc::set_smem_limit<xattn_tc_kernel<DP>>(Cfg<DP>::SMEM);
+    if (e != cudaSuccess) return e;
+    xattn_tc_kernel<DP><<<(unsigned)std::min<int64_t>(p.items, sms), NUM_THREADS, Cfg<DP>::SMEM, s>>>(p, tq, tk, tv);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+bool xattn_tc_supported(const XAttnArgs& a) {
+    const auto ok16 = [](const void* p) { return ((uintptr_t)p & 15) == 0; };
+    const int g = a.H / a.Hkv;
+    uint64_t unused;
+    return a.dtype == VD_BF16 && a.D % 8 == 0 && a.D <= 128 && g <= ROWS && a.Tk >= 1 && ok16(a.q) && ok16(a.k) && ok16(a.v) && ok16(a.o) &&
+           ((a.so.batch | a.so.token | a.so.head) & 7) == 0 && stride_ok(a.sq.head, a.H, &unused) && stride_ok(a.sq.token, a.Tq, &unused) &&
+           stride_ok(a.sq.batch, a.B, &unused) && stride_ok(a.sk.token, a.Tk, &unused) && stride_ok(a.sv.token, a.Tk, &unused) &&
+           ((a.sk.head | a.sk.batch | a.sv.head | a.sv.batch) & 7) == 0 && a.sq.head < (1ll << 38) / std::max(g, 1);
+}
+
+cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s) {
+    CUtensorMap tq, tk, tv;
+    Params p;
+    p.o = a.o; p.lens = a.kv_lens;
+    p.Tq = a.Tq; p.Tk = a.Tk; p.Hkv = a.Hkv; p.g = a.H / a.Hkv; p.D = a.D; p.nt = ROWS / p.g;
+    p.q_items = (a.Tq + 2 * p.nt - 1) / (2 * p.nt);
+    p.items = (int64_t)p.q_items * a.Hkv * a.B;
+    p.o_batch = a.so.batch; p.o_token = a.so.token; p.o_head = a.so.head;
+    p.scale_log2 = a.scale * 1.4426950408889634f;
+    const uint64_t dims[5] = {(uint64_t)a.D, (uint64_t)p.g, (uint64_t)a.Tq, (uint64_t)a.Hkv, (uint64_t)a.B};
+    uint64_t st[4];
+    const uint32_t box[5] = {CHUNK, (uint32_t)p.g, (uint32_t)p.nt, 1, 1};
+    if (!stride_ok(a.sq.head, p.g, &st[0]) || !stride_ok(a.sq.token, a.Tq, &st[1]) || !stride_ok(a.sq.head * p.g, a.Hkv, &st[2]) ||
+        !stride_ok(a.sq.batch, a.B, &st[3]) || !encode(&tq, a.q, 5, dims, st, box) || !encode_kv(&tk, a, a.k, a.sk, &p.kh, &p.kb) ||
+        !encode_kv(&tv, a, a.v, a.sv, &p.vh, &p.vb))
+        return cudaErrorInvalidValue;
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    return a.D <= 64 ? launch<64>(p, tq, tk, tv, sms, s) : launch<128>(p, tq, tk, tv, sms, s);
+}
+
+}  // namespace vd
