@@ -66,8 +66,12 @@ vd_status vd_op_cross_attention(const vd_xattn_desc* d, const void* q, const voi
     XAttnArgs a{q, k, v, o, kv_lens, d->dtype, d->batch, d->q_len, d->kv_len, d->heads, d->kv_heads, d->head_dim,
                 {d->q_batch, d->q_token, d->q_head}, {d->k_batch, d->k_token, d->k_head}, {d->v_batch, d->v_token, d->v_head},
                 {d->o_batch, d->o_token, d->o_head}, d->scale};
-    const bool tc = d->impl == VD_XATTN_AUTO && (int64_t)d->q_len * (d->heads / d->kv_heads) > 8 && xattn_tc_supported(a);
-    return done(tc ? launch_xattn_tc(a, (cudaStream_t)cuda_stream) : launch_xattn_plain(a, (cudaStream_t)cuda_stream), "vd_op_cross_attention");
+    const int64_t rows = (int64_t)d->q_len * (d->heads / d->kv_heads);       // of a key head
+    cudaError_t e;
+    if (d->impl == VD_XATTN_AUTO && rows <= 16 && xattn_rows_supported(a)) e = launch_xattn_rows(a, (cudaStream_t)cuda_stream);
+    else if (d->impl == VD_XATTN_AUTO && xattn_tc_supported(a)) e = launch_xattn_tc(a, (cudaStream_t)cuda_stream);
+    else e = launch_xattn_plain(a, (cudaStream_t)cuda_stream);
+    return done(e, "vd_op_cross_attention");
 }
 
 static const char* rotary_axes_error(int rotary_dim, int axes, const int32_t* pairs) {

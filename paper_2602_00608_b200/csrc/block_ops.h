@@ -19,6 +19,8 @@ struct XAttnArgs {
     float scale;
 };
 cudaError_t launch_xattn_plain(const XAttnArgs& a, cudaStream_t s);
+bool xattn_rows_supported(const XAttnArgs& a);
+cudaError_t launch_xattn_rows(const XAttnArgs& a, cudaStream_t s);
 bool xattn_tc_supported(const XAttnArgs& a);
 cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s);
 

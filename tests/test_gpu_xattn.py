@@ -41,7 +41,7 @@ SIZES = [  # b, tq, tk, h, hkv, d
     (1, 1, 1, 1, 1, 64), (2, 1, 7, 4, 4, 64), (3, 1, 130, 8, 2, 128), (2, 3, 300, 6, 2, 80), (1, 17, 33, 5, 5, 40), (2, 64, 77, 3, 3, 64),
     (1, 127, 129, 2, 2, 128), (2, 128, 128, 2, 1, 64), (1, 129, 127, 4, 2, 96), (1, 255, 256, 3, 1, 128), (2, 257, 385, 2, 2, 72), (1, 300, 1, 2, 2, 64),
     (1, 513, 640, 2, 1, 32), (1, 1, 2049, 8, 1, 128), (1, 2, 5000, 4, 4, 64), (5, 31, 511, 7, 7, 128), (1, 40, 700, 30, 6, 64), (1, 9, 100, 16, 1, 128),
-    (1, 130, 260, 3, 3, 256), (2, 5, 50, 2, 2, 1), (1, 19, 21, 2, 1, 7), (1, 70, 200, 2, 2, 160), (1, 20, 90, 1, 1, 255)]
+    (1, 130, 260, 3, 3, 256), (2, 5, 50, 2, 2, 1), (1, 16, 300, 2, 2, 128), (2, 1, 1000, 10, 1, 64), (1, 11, 77, 1, 1, 40), (1, 4, 500, 8, 4, 96), (3, 2, 4100, 12, 2, 128), (1, 8, 17, 2, 2, 72), (2, 1, 900, 3, 1, 256), (1, 19, 21, 2, 1, 7), (1, 70, 200, 2, 2, 160), (1, 20, 90, 1, 1, 255)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
