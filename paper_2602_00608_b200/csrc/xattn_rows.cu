@@ -7,18 +7,20 @@
 // weights).  With more rows the arithmetic is what bounds this, and bf16 takes matrix instructions instead (below).  Warps meet in shared memory; where there are few heads, a cluster of up to eight CTAs divides the keys and meets in
 // distributed shared memory.  Fixed orders throughout: the same bits each time.
 #include <algorithm>
+#include <mutex>
 
 #include "block_ops.h"
 #include "conv_cluster.cuh"
 #include "tc_common.cuh"
 #include "tc_pair.cuh"
+#include "xattn_maps.h"
 
 namespace vd {
 namespace {
 
 using namespace tc;
 
-constexpr int WARPS = 8, MAX_SPLITS = 8;
+constexpr int MAX_SPLITS = 8;
 constexpr float RESCALE_THRESHOLD = 8.0f;
 
 struct RowParams {
@@ -98,7 +100,7 @@ template <int R> __device__ __forceinline__ Work work_of(const RowParams& p) {
     return w;
 }
 // shared memory: the warps' accumulators, the CTA's, and (maximum, sum) of either; `rows` rows of DM channels each
-template <int DM> struct Shared {
+template <int DM, int WARPS> struct Shared {
     float* base;
     int rows;
     __device__ __forceinline__ Shared(float* b, int r) : base(b), rows(r) {}
@@ -107,13 +109,13 @@ template <int DM> struct Shared {
     __device__ __forceinline__ float2* ml(int warp, int r) const { return (float2*)acc(WARPS + 1, 0) + warp * rows + r; }
     __device__ __forceinline__ float2* om(int r) const { return ml(WARPS, r); }
 };
-constexpr int shared_bytes(int rows, int dm) { return (WARPS + 1) * rows * (dm + 2) * 4; }
+constexpr int shared_bytes(int warps, int rows, int dm) { return (warps + 1) * rows * (dm + 2) * 4; }
 
 // The warps' shares are in shared memory: added up and written, or left there for the cluster, whose CTAs each finish a part.
-template <typename T, int DM> __device__ __forceinline__ void meet(const RowParams& p, const Shared<DM>& sh, const Work& w, int split, int tid) {
+template <typename T, int DM, int WARPS> __device__ __forceinline__ void meet(const RowParams& p, const Shared<DM, WARPS>& sh, const Work& w, int split, int tid) {
     const XAttnArgs& a = p.a;
     __syncthreads();
-    for (int i = tid; i < w.rows * DM; i += WARPS * 32) {
+    for (int i = tid; i < w.rows * DM && tid < WARPS * 32; i += WARPS * 32) {
         const int r = i / DM, d = i % DM;
         float2 ml[WARPS];
         float m = -INFINITY;
@@ -139,7 +141,7 @@ template <typename T, int DM> __device__ __forceinline__ void meet(const RowPara
     }
     if (p.splits == 1) return;
     cluster_sync_all();                                      // every CTA's share is in its shared memory
-    for (int i = split * (WARPS * 32) + tid; i < w.rows * DM; i += p.splits * WARPS * 32) {
+    for (int i = split * (WARPS * 32) + tid; i < w.rows * DM && tid < WARPS * 32; i += p.splits * WARPS * 32) {
         const int r = i / DM, d = i % DM;
         if (d >= a.D) continue;
         float m[MAX_SPLITS], sum[MAX_SPLITS], o[MAX_SPLITS], top = -INFINITY;
@@ -165,13 +167,13 @@ template <typename T, int DM> __device__ __forceinline__ void meet(const RowPara
     cluster_sync_all();                                      // nobody leaves while others read its memory
 }
 
-template <typename T, int R, int U, int LPK, int NVL>
+template <typename T, int R, int U, int LPK, int NVL, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32, 2) xattn_rows_kernel(const RowParams p) {
     constexpr int E = Vec<T>::E, P = E / 2, N = R * U, KPL = 32 / LPK, KPI = KPL * U, SPAN = LPK * E;     // KPI: keys of a warp's round
     constexpr int DUP = LPK / N, DM = SPAN * NVL;            // DUP: lanes that hold the same score; DM: channels that are held
     static_assert(N <= LPK, "");
     extern __shared__ float smem[];
-    const Shared<DM> sh(smem, R);
+    const Shared<DM, WARPS> sh(smem, R);
     const XAttnArgs& a = p.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, x = lane % LPK, kg = lane / LPK;
     const int split = p.splits > 1 ? (int)cluster_ctarank() : 0;
@@ -293,183 +295,245 @@ __global__ void __launch_bounds__(WARPS * 32, 2) xattn_rows_kernel(const RowPara
                 }
                 if (kg == 0) *(float2*)(sh.acc(warp, r) + n * SPAN + x * E + 2 * i) = make_float2(f0, f1);
             }
-    meet<T, DM>(p, sh, w, split, tid);
+    meet<T, DM, WARPS>(p, sh, w, split, tid);
 }
 
-// bf16, up to 16 rows: scores and products on the matrix instructions (mma m16n8k16; with this few rows the bytes bound the call, and
-// operands go from memory to registers as they are).  Rows are the products' narrow side, eight at a time.  A lane
-// (g, c) = (lane / 4, lane % 4):
-//   S^T = K Q^T    holds 16-byte chunks c, c + 4, ... of keys g and g + 8: a chunk's first two words are its share of one product, the
-//                  others of the next, and Q's chunks are taken alike, so the channels' order does not matter
-//   O^T = V^T P^T  P^T is S^T as the products left it, turned by movmatrix; holds chunks g (+ 8) of keys 2c, 2c + 1, 2c + 8, 2c + 9: product i
-//                  takes channels 2i and 2i + 1 of every chunk, pairs of keys put together by byte permutes
-// The next round's k loads go out once k is in the scores, those of v once v is in the output.
-__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+// bf16, up to 16 rows: scores and products on the matrix instructions (mma m16n8k16: with this few rows the bytes bound the call, not
+// the products), k and v through a ring of shared-memory stages that one thread keeps filled by bulk tensor loads: up to 192 KB
+// of an SM under way.  Rows are the products' narrow side, eight at a time:
+//   S^T = K Q^T      K by ldmatrix as it lies in the stage, Q in registers
+//   O^T = V^T P^T    V by transposing ldmatrix, P^T is S^T as the products left it, turned by movmatrix
+// A warp takes 16 keys of every stage and keeps a maximum, a sum and an output of its own.
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
     uint32_t r;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-// DC: 64-channel groups; KB: blocks of 16 keys of a warp's round; NR: groups of eight rows
-template <int DC, int KB, int NR>
-__global__ void __launch_bounds__(WARPS * 32) xattn_rows_mma_kernel(const RowParams p) {
-    constexpr int R = NR * 8, DM = DC * 64, QC = DC * 2;     // QC: Q and K chunks of a lane
-    extern __shared__ float smem[];
-    const Shared<DM> sh(smem, R);
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+constexpr int STREAM_WARPS = 8, STREAM_KEYS = STREAM_WARPS * 16, STREAM_THREADS = (STREAM_WARPS + 1) * 32;
+template <int DP> struct StreamCfg {
+    static constexpr int STAGES = DP == 128 ? 3 : 6, TILE = STREAM_KEYS * DP * 2, SMEM = STAGES * 2 * TILE + 128 + 1024;
+    static_assert(SMEM <= 232448 && shared_bytes(STREAM_WARPS, 16, DP) <= STAGES * 2 * TILE, "shared memory of one CTA; the meeting's lies over the stages");
+};
+struct StreamBars { uint64_t full[6], empty[6]; uint32_t abort_flag; };
+static_assert(sizeof(StreamBars) <= 128, "");
+struct StreamParams {
+    RowParams p;
+    int kb, vb, kh, vh;          // 0: the batch (head) coordinate of k or v stays 0
+};
+// NR: groups of eight rows
+template <int DP, int NR>
+__global__ void __launch_bounds__(STREAM_THREADS, 1)
+xattn_stream_kernel(const StreamParams sp, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
+    using C = StreamCfg<DP>;
+    constexpr int R = NR * 8, KS = DP / 16;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* stages = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    StreamBars* bars = (StreamBars*)(stages + C::STAGES * 2 * C::TILE);
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+    const RowParams& p = sp.p;
     const XAttnArgs& a = p.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+    if (tid == 0) {
+        for (int i = 0; i < C::STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), STREAM_WARPS); }
+        bars->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async_smem();
+    }
+    __syncthreads();
     const int split = p.splits > 1 ? (int)cluster_ctarank() : 0;
     const Work w = work_of<R>(p);
-    const int chunks = a.D / 8;
-    const uint4 zero = make_uint4(0, 0, 0, 0);
-    uint4 q[NR][QC];                                         // row 8 n + g
-#pragma unroll
-    for (int n = 0; n < NR; ++n)
-#pragma unroll
-        for (int j = 0; j < QC; ++j)
-            q[n][j] = c + 4 * j < chunks && n * 8 + g < w.rows ? *(const uint4*)((const __nv_bfloat16*)a.q + w.at(p, a.sq, n * 8 + g) + (c + 4 * j) * 8) : zero;
-    const __nv_bfloat16* k = (const __nv_bfloat16*)a.k + w.b * a.sk.batch + w.kvh * a.sk.head + c * 8;
-    const __nv_bfloat16* v = (const __nv_bfloat16*)a.v + w.b * a.sv.batch + w.kvh * a.sv.head + g * 8;
-    float o[DC][4][NR][4] = {};
-    float m[NR][2], l[NR][2];                                // of rows 8 n + 2c, + 1
+    const int tiles = (w.len + STREAM_KEYS - 1) / STREAM_KEYS, mine = tiles > split ? (tiles - split + p.splits - 1) / p.splits : 0;
+    const Shared<DP, STREAM_WARPS> sh((float*)stages, R);
+    float o[KS][NR][4] = {};                                 // channels 16 i + g, + 8 of rows 8 n + 2c, + 1
+    float m[NR][2], l[NR][2];
 #pragma unroll
     for (int n = 0; n < NR; ++n) { m[n][0] = m[n][1] = -INFINITY; l[n][0] = l[n][1] = 0.f; }
-    uint4 kr[KB][2][QC], vr[KB][4][DC];
-    auto load_k = [&](int base) {
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int key = base + kb * 16 + h * 8 + g;
-                const __nv_bfloat16* at = k + key * a.sk.token;
-#pragma unroll
-                for (int j = 0; j < QC; ++j) {
-                    kr[kb][h][j] = zero;
-                    if (key < w.len && c + 4 * j < chunks) kr[kb][h][j] = ldg_stream(at + j * 32);
+    if (warp == STREAM_WARPS) {
+        if (lane == 0) {
+            bool ok = true;
+            int i = 0;
+            for (; i < mine && ok; ++i) {
+                const int st = i % C::STAGES, tile = split + i * p.splits;
+                ok = mbar_wait(smem_u32(&bars->empty[st]), ((i / C::STAGES) & 1) ^ 1, abort_flag);
+                if (!ok) break;
+                const uint32_t full = smem_u32(&bars->full[st]), dst = smem_u32(stages + st * 2 * C::TILE);
+                mbar_arrive_expect_tx(full, 2 * C::TILE);
+                for (int x = 0; x < DP / 64; ++x) {
+                    tma_load_4d(dst + x * (STREAM_KEYS * 128), &tm_k, x * 64, tile * STREAM_KEYS, w.kvh * sp.kh, w.b * sp.kb, full);
+                    tma_load_4d(dst + C::TILE + x * (STREAM_KEYS * 128), &tm_v, x * 64, tile * STREAM_KEYS, w.kvh * sp.vh, w.b * sp.vb, full);
                 }
             }
-    };
-    auto load_v = [&](int base) {
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int key = base + kb * 16 + 2 * c + (i & 1) + (i >> 1) * 8;
-                const __nv_bfloat16* at = v + key * a.sv.token;
-#pragma unroll
-                for (int dc = 0; dc < DC; ++dc) {
-                    vr[kb][i][dc] = zero;
-                    if (key < w.len && dc * 8 + g < chunks) vr[kb][i][dc] = ldg_stream(at + dc * 64);
-                }
-            }
-    };
-    const int step = p.splits * WARPS * (KB * 16);
-    int base = (split * WARPS + warp) * (KB * 16);           // (below 2^31: a round reaches at most 2^15 keys further than the last key)
-    if (base < w.len) { load_k(base); load_v(base); }
-    for (; base < w.len; base += step) {
-        float s[KB][NR][4];                                  // keys g (first two) and g + 8 of rows 8 n + 2c, + 1
-        bool grow = false;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                float d0[4] = {0.f, 0.f, 0.f, 0.f}, d1[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int j = 0; j < QC; ++j) {
-                    const uint4 x = kr[kb][0][j], y = kr[kb][1][j];
-                    mma_16816(d0, x.x, y.x, x.y, y.y, q[n][j].x, q[n][j].y);
-                    mma_16816(d1, x.z, y.z, x.w, y.w, q[n][j].z, q[n][j].w);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[kb][n][e] = base + kb * 16 + (e >> 1) * 8 + g < w.len ? (d0[e] + d1[e]) * p.scale_log2 : -INFINITY;
-                    grow = grow || s[kb][n][e] > m[n][e & 1] + RESCALE_THRESHOLD;
-                }
-            }
+            if (!ok || *abort_flag) cc::land_loads(bars->full, C::STAGES, i);     // (else the others wait for all of them)
         }
-        const bool more = base + step < w.len;
-        if (more) load_k(base + step);
-        if (__any_sync(0xffffffffu, grow)) {
+        __syncwarp();
+    } else {
+        uint32_t q[KS][NR][2];                               // row 8 n + g, channels 16 k + 2c, + 1 and + 8, + 9
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float top = m[n][e];
-#pragma unroll
-                    for (int kb = 0; kb < KB; ++kb) top = fmaxf(top, fmaxf(s[kb][n][e], s[kb][n][e + 2]));
-#pragma unroll
-                    for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                    const float f = top == -INFINITY ? 1.f : ex2(m[n][e] - top);
-                    m[n][e] = top;
-                    l[n][e] *= f;
-#pragma unroll
-                    for (int dc = 0; dc < DC; ++dc)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) { o[dc][i][n][e] *= f; o[dc][i][n][e + 2] *= f; }
+                for (int h = 0; h < 2; ++h) {
+                    const int ch = k * 16 + h * 8 + 2 * c;
+                    q[k][n][h] = ch < a.D && n * 8 + g < w.rows ? *(const uint32_t*)((const __nv_bfloat16*)a.q + w.at(p, a.sq, n * 8 + g) + ch) : 0u;
                 }
-        }
+        // addresses within a tile: lane's row of the four 8x8 matrices; 16-byte chunk x of row r lies at x ^ (r & 7)
+        const int k_row = warp * 16 + (lane & 7) + ((lane >> 3) & 1) * 8, v_row = warp * 16 + (lane & 7) + (lane >> 4) * 8;
+        const uint32_t k_at = (uint32_t)(k_row * 128), v_at = (uint32_t)(v_row * 128), k_hi = (uint32_t)(lane >> 4), v_hi = (uint32_t)((lane >> 3) & 1), sw = (uint32_t)(lane & 7);
+        bool ok = true;
+        for (int i = 0; i < mine; ++i) {
+            const int st = i % C::STAGES, left = w.len - (split + i * p.splits) * STREAM_KEYS - warp * 16;       // keys of this warp's 16 that count
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->full[st]), (i / C::STAGES) & 1, abort_flag)) && ok;
+            if (left > 0) {
+                const uint32_t kt = smem_u32(stages + st * 2 * C::TILE) + k_at, vt = smem_u32(stages + st * 2 * C::TILE + C::TILE) + v_at;
+                if (left < 16) {                             // 0 * NaN is NaN: values that do not count become zeros (the last stage: never filled again)
+                    for (int x = lane; x < (16 - left) * 8; x += 32)
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-            uint32_t b0[NR], b1[NR];
+                        for (int y = 0; y < DP / 64; ++y)
+                            *(uint4*)(stages + st * 2 * C::TILE + C::TILE + y * (STREAM_KEYS * 128) + (warp * 16 + left) * 128 + x * 16) = make_uint4(0, 0, 0, 0);
+                    __syncwarp();
+                }
+                float s[NR][4], s1[NR][4];                   // keys g (first two) and g + 8 of rows 8 n + 2c, + 1
 #pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                const float r0 = m[n][0] == -INFINITY ? 0.f : m[n][0], r1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
-                const float e0 = ex2(s[kb][n][0] - r0), e1 = ex2(s[kb][n][1] - r1), e2 = ex2(s[kb][n][2] - r0), e3 = ex2(s[kb][n][3] - r1);
-                l[n][0] += e0 + e2;
-                l[n][1] += e1 + e3;
-                b0[n] = transpose_8x8(pack_bf16(e0, e1));
-                b1[n] = transpose_8x8(pack_bf16(e2, e3));
-            }
+                for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int dc = 0; dc < DC; ++dc) {
-                const uint4 x0 = vr[kb][0][dc], x1 = vr[kb][1][dc], x2 = vr[kb][2][dc], x3 = vr[kb][3][dc];
-                const uint32_t w0[4] = {x0.x, x0.y, x0.z, x0.w}, w1[4] = {x1.x, x1.y, x1.z, x1.w}, w2[4] = {x2.x, x2.y, x2.z, x2.w}, w3[4] = {x3.x, x3.y, x3.z, x3.w};
+                    for (int e = 0; e < 4; ++e) s[n][e] = s1[n][e] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t a0 = __byte_perm(w0[i], w1[i], 0x5410), a1 = __byte_perm(w0[i], w1[i], 0x7632),
-                                   a2 = __byte_perm(w2[i], w3[i], 0x5410), a3 = __byte_perm(w2[i], w3[i], 0x7632);
+                for (int k = 0; k < KS; ++k) {
+                    uint32_t f[4];
+                    ldsm4(f, kt + (uint32_t)((k >> 2) * (STREAM_KEYS * 128)) + (((uint32_t)((k & 3) * 2) + k_hi) ^ sw) * 16u);
 #pragma unroll
-                    for (int n = 0; n < NR; ++n) mma_16816(o[dc][i][n], a0, a1, a2, a3, b0[n], b1[n]);
+                    for (int n = 0; n < NR; ++n) mma_16816(k & 1 ? s1[n] : s[n], f, q[k][n][0], q[k][n][1]);
+                }
+                bool grow = false;
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[n][e] = (e >> 1) * 8 + g < left ? (s[n][e] + s1[n][e]) * p.scale_log2 : -INFINITY;
+                        grow = grow || s[n][e] > m[n][e & 1] + RESCALE_THRESHOLD;
+                    }
+                if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                    for (int n = 0; n < NR; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float top = fmaxf(m[n][e], fmaxf(s[n][e], s[n][e + 2]));
+#pragma unroll
+                            for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                            const float f = top == -INFINITY ? 1.f : ex2(m[n][e] - top);
+                            m[n][e] = top;
+                            l[n][e] *= f;
+#pragma unroll
+                            for (int k = 0; k < KS; ++k) { o[k][n][e] *= f; o[k][n][e + 2] *= f; }
+                        }
+                }
+                uint32_t b0[NR], b1[NR];
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                    const float r0 = m[n][0] == -INFINITY ? 0.f : m[n][0], r1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
+                    const float e0 = ex2(s[n][0] - r0), e1 = ex2(s[n][1] - r1), e2 = ex2(s[n][2] - r0), e3 = ex2(s[n][3] - r1);
+                    l[n][0] += e0 + e2;
+                    l[n][1] += e1 + e3;
+                    b0[n] = transpose_8x8(pack_bf16(e0, e1));
+                    b1[n] = transpose_8x8(pack_bf16(e2, e3));
+                }
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    uint32_t f[4];
+                    ldsm4_t(f, vt + (uint32_t)((k >> 2) * (STREAM_KEYS * 128)) + (((uint32_t)((k & 3) * 2) + v_hi) ^ sw) * 16u);
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) mma_16816(o[k][n], f, b0[n], b1[n]);
                 }
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars->empty[st]));
         }
-        if (more) load_v(base + step);
+        if (!ok) l[0][0] = l[0][1] = l[NR - 1][0] = l[NR - 1][1] = __int_as_float(0x7fffffff);
     }
+    __syncthreads();                                         // every load has landed and been used: the stages become the meeting's memory
+    if (warp < STREAM_WARPS) {
 #pragma unroll
-    for (int n = 0; n < NR; ++n)
+        for (int n = 0; n < NR; ++n)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+            for (int e = 0; e < 2; ++e) {
 #pragma unroll
-            for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], d);
-            if (g == 0) *sh.ml(warp, n * 8 + 2 * c + e) = make_float2(m[n][e], l[n][e]);
+                for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], d);
+                if (g == 0) *sh.ml(warp, n * 8 + 2 * c + e) = make_float2(m[n][e], l[n][e]);
 #pragma unroll
-            for (int dc = 0; dc < DC; ++dc)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *(float2*)(sh.acc(warp, n * 8 + 2 * c + e) + (dc * 8 + g) * 8 + 2 * i) = make_float2(o[dc][i][n][e], o[dc][i][n][e + 2]);
-        }
-    meet<__nv_bfloat16, DM>(p, sh, w, split, tid);
+                for (int k = 0; k < KS; ++k) {
+                    sh.acc(warp, n * 8 + 2 * c + e)[k * 16 + g] = o[k][n][e];
+                    sh.acc(warp, n * 8 + 2 * c + e)[k * 16 + g + 8] = o[k][n][e + 2];
+                }
+            }
+    }
+    meet<__nv_bfloat16, DP, STREAM_WARPS>(p, sh, w, split, tid);
 }
 
-// KERNEL for groups of `rows` rows, `round` keys of a CTA at a time
-template <auto KERNEL> cudaError_t launch_split(const XAttnArgs& a, int rows, int dm, int round, cudaStream_t s) {
+// clusters of `splits` CTAs of KERNEL that the current device holds at once (0: none), asked once per device
+template <auto KERNEL> int clusters_held(int threads, int smem, int splits) {
+    static std::mutex mu;
+    static int known[cc::kMaxDevices][MAX_SPLITS] = {};      // 0: not asked, else the answer + 1
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= cc::kMaxDevices || cc::set_smem_limit<KERNEL>(smem) != cudaSuccess) {
+        cudaGetLastError();
+        return 0;
+    }
+    std::lock_guard<std::mutex> lock(mu);
+    int& k = known[dev][splits - 1];
+    if (k == 0) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)splits);
+        cfg.blockDim = dim3((unsigned)threads);
+        cfg.dynamicSmemBytes = (size_t)smem;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)splits; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, (const void*)KERNEL, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
+        k = n + 1;
+    }
+    return k - 1;
+}
+
+// CTAs that share the keys of a group: the fewest waves of clusters x (rounds of a CTA + what a CTA costs besides, in rounds)
+template <auto KERNEL> RowParams plan_rows(const XAttnArgs& a, int threads, int rows, int smem, int round) {
     RowParams p{a, a.H / a.Hkv, 0, 1, a.scale * 1.4426950408889634f};
     p.groups = (int)(((int64_t)a.Tq * p.g + rows - 1) / rows);
     const int64_t items = (int64_t)p.groups * a.Hkv * a.B;
-    const int smem = shared_bytes(rows, dm);
-    // two CTAs per SM; a split has at least one round of keys for each of its warps
-    while (p.splits < MAX_SPLITS && items * p.splits < 148 && a.Tk > p.splits * round && cc::clusters_fit<KERNEL>(WARPS * 32, smem, 2 * p.splits)) p.splits *= 2;
-    return cc::launch_clusters<KERNEL>({items * p.splits, WARPS * 32, smem, smem, p.splits}, s, p);
+    double best = 0.0;
+    for (int n = 1; n <= MAX_SPLITS && (n == 1 || (n - 1) * round < a.Tk); ++n) {
+        const int held = clusters_held<KERNEL>(threads, smem, n);
+        if (held < 1) continue;
+        const double cost = (double)((items + held - 1) / held) * ((a.Tk + n * round - 1) / (n * round) + (n == 1 ? 2.0 : 3.0));
+        if (best == 0.0 || cost < best) { best = cost; p.splits = n; }
+    }
+    return p;
 }
 template <typename T, int R, int U, int LPK, int NVL> cudaError_t launch(const XAttnArgs& a, cudaStream_t s) {
-    return launch_split<xattn_rows_kernel<T, R, U, LPK, NVL>>(a, R, LPK * Vec<T>::E * NVL, 32 / LPK * U * WARPS, s);
+    constexpr int W = 8, smem = shared_bytes(W, R, LPK * Vec<T>::E * NVL);
+    const RowParams p = plan_rows<xattn_rows_kernel<T, R, U, LPK, NVL, W>>(a, W * 32, R, smem, 32 / LPK * U * W);
+    return cc::launch_clusters<xattn_rows_kernel<T, R, U, LPK, NVL, W>>({(int64_t)p.groups * a.Hkv * a.B * p.splits, W * 32, smem, smem, p.splits}, s, p);
 }
-template <int DC, int KB> cudaError_t launch_mma(const XAttnArgs& a, int64_t rows, cudaStream_t s) {
-    return rows <= 8 ? launch_split<xattn_rows_mma_kernel<DC, KB, 1>>(a, 8, DC * 64, KB * 16 * WARPS, s)
-                     : launch_split<xattn_rows_mma_kernel<DC, KB, 2>>(a, 16, DC * 64, KB * 16 * WARPS, s);
+template <int DP, int NR> cudaError_t launch_stream(const XAttnArgs& a, cudaStream_t s) {
+    constexpr int smem = StreamCfg<DP>::SMEM;
+    CUtensorMap tk, tv;
+    StreamParams sp;
+    if (!encode_kv(&tk, a, a.k, a.sk, STREAM_KEYS, &sp.kh, &sp.kb) || !encode_kv(&tv, a, a.v, a.sv, STREAM_KEYS, &sp.vh, &sp.vb)) return cudaErrorInvalidValue;
+    sp.p = plan_rows<xattn_stream_kernel<DP, NR>>(a, STREAM_THREADS, NR * 8, smem, STREAM_KEYS);
+    return cc::launch_clusters<xattn_stream_kernel<DP, NR>>({(int64_t)sp.p.groups * a.Hkv * a.B * sp.p.splits, STREAM_THREADS, smem, smem, sp.p.splits}, s, sp, tk, tv);
 }
 
 template <typename T, int R> cudaError_t launch_rows(const XAttnArgs& a, cudaStream_t s) {
@@ -493,8 +557,14 @@ bool xattn_rows_supported(const XAttnArgs& a) {
 cudaError_t launch_xattn_rows(const XAttnArgs& a, cudaStream_t s) {
     const int64_t rows = (int64_t)a.Tq * (a.H / a.Hkv);
     if (a.dtype == VD_BF16) {
-        if (rows == 1 || a.D > 128) return rows == 1 ? launch_rows<__nv_bfloat16, 1>(a, s) : rows == 2 ? launch_rows<__nv_bfloat16, 2>(a, s) : launch_rows<__nv_bfloat16, 4>(a, s);
-        return a.D <= 64 ? launch_mma<1, 2>(a, rows, s) : launch_mma<2, 1>(a, rows, s);
+        // One row: few heads with long contexts want the ring's bytes in flight, many heads have them anyway and short contexts end
+        // sooner without it (us, lanes / ring: 16 heads x 16000 keys of 64 23.5 / 16.6, 4 x 8000 of 128, 4 rows 33.7 / 12.5; 256 x 2000 43.1 / 45.4,
+        // 32 x 100 4.8 / 6.5).  Two to four rows: 256 x 2000, two rows 48.0 / 45.8, 32 x 16384, four rows 103 / 47.
+        if ((rows > 1 || (a.Tk > 1024 && (int64_t)a.B * a.Hkv < 148)) && kv_maps_supported(a)) {
+            if (a.D <= 64) return rows <= 8 ? launch_stream<64, 1>(a, s) : launch_stream<64, 2>(a, s);
+            return rows <= 8 ? launch_stream<128, 1>(a, s) : launch_stream<128, 2>(a, s);
+        }
+        return rows == 1 ? launch_rows<__nv_bfloat16, 1>(a, s) : rows == 2 ? launch_rows<__nv_bfloat16, 2>(a, s) : launch_rows<__nv_bfloat16, 4>(a, s);
     }
     return rows == 1 ? launch_rows<float, 1>(a, s) : rows == 2 ? launch_rows<float, 2>(a, s) : launch_rows<float, 4>(a, s);
 }

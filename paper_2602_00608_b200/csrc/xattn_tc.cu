@@ -18,6 +18,7 @@
 #include "block_ops.h"
 #include "conv_cluster.cuh"
 #include "tc_common.cuh"
+#include "xattn_maps.h"
 
 namespace vd {
 namespace {
@@ -407,32 +408,6 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
     }
 }
 
-bool encode(CUtensorMap* tm, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes, const uint32_t* box) {
-    EncodeTiledFn enc = encode_fn();
-    if (!enc) return false;
-    cuuint64_t d[5], st[4];
-    cuuint32_t bx[5], es[5];
-    for (int i = 0; i < rank; ++i) { d[i] = dims[i]; bx[i] = box[i]; es[i] = 1; }
-    for (int i = 0; i + 1 < rank; ++i) st[i] = strides_bytes[i];
-    return enc(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, st, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-// bytes between the elements of a dimension; one that is never stepped along gets any valid stride
-bool stride_ok(int64_t stride, int64_t n, uint64_t* bytes) {
-    if (n <= 1) { *bytes = 256; return true; }
-    *bytes = (uint64_t)stride * 2;
-    return stride > 0 && stride % 8 == 0 && stride < (1ll << 38);
-}
-// k or v as [D, keys, heads, batch]; where a stride is 0 the coordinate stays 0
-bool encode_kv(CUtensorMap* tm, const XAttnArgs& a, const void* p, const Strides& s, int* use_head, int* use_batch) {
-    *use_head = s.head != 0;
-    *use_batch = s.batch != 0;
-    const uint64_t dims[4] = {(uint64_t)a.D, (uint64_t)a.Tk, s.head ? (uint64_t)a.Hkv : 1, s.batch ? (uint64_t)a.B : 1};
-    uint64_t st[3];
-    const uint32_t box[4] = {CHUNK, KEYS, 1, 1};
-    return stride_ok(s.token, dims[1], &st[0]) && stride_ok(s.head, dims[2], &st[1]) && stride_ok(s.batch, dims[3], &st[2]) && encode(tm, p, 4, dims, st, box);
-}
-
 template <int DP> cudaError_t launch(const Params& p, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, int sms, cudaStream_t s) {
     const cudaError_t e = cc::set_smem_limit<xattn_tc_kernel<DP>>(Cfg<DP>::SMEM);
     if (e != cudaSuccess) return e;
@@ -443,13 +418,11 @@ template <int DP> cudaError_t launch(const Params& p, const CUtensorMap& tq, con
 }  // namespace
 
 bool xattn_tc_supported(const XAttnArgs& a) {
-    const auto ok16 = [](const void* p) { return ((uintptr_t)p & 15) == 0; };
     const int g = a.H / a.Hkv;
     uint64_t unused;
-    return a.dtype == VD_BF16 && a.D % 8 == 0 && a.D <= 128 && g <= ROWS && a.Tk >= 1 && ok16(a.q) && ok16(a.k) && ok16(a.v) && ok16(a.o) &&
-           ((a.so.batch | a.so.token | a.so.head) & 7) == 0 && stride_ok(a.sq.head, a.H, &unused) && stride_ok(a.sq.token, a.Tq, &unused) &&
-           stride_ok(a.sq.batch, a.B, &unused) && stride_ok(a.sk.token, a.Tk, &unused) && stride_ok(a.sv.token, a.Tk, &unused) &&
-           ((a.sk.head | a.sk.batch | a.sv.head | a.sv.batch) & 7) == 0 && a.sq.head < (1ll << 38) / std::max(g, 1);
+    return kv_maps_supported(a) && g <= ROWS && (((uintptr_t)a.q | (uintptr_t)a.o) & 15) == 0 && ((a.so.batch | a.so.token | a.so.head) & 7) == 0 &&
+           stride_ok(a.sq.head, a.H, &unused) && stride_ok(a.sq.token, a.Tq, &unused) && stride_ok(a.sq.batch, a.B, &unused) &&
+           a.sq.head < (1ll << 38) / std::max(g, 1);
 }
 
 cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s) {
@@ -465,8 +438,8 @@ cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s) {
     uint64_t st[4];
     const uint32_t box[5] = {CHUNK, (uint32_t)p.g, (uint32_t)p.nt, 1, 1};
     if (!stride_ok(a.sq.head, p.g, &st[0]) || !stride_ok(a.sq.token, a.Tq, &st[1]) || !stride_ok(a.sq.head * p.g, a.Hkv, &st[2]) ||
-        !stride_ok(a.sq.batch, a.B, &st[3]) || !encode(&tq, a.q, 5, dims, st, box) || !encode_kv(&tk, a, a.k, a.sk, &p.kh, &p.kb) ||
-        !encode_kv(&tv, a, a.v, a.sv, &p.vh, &p.vb))
+        !stride_ok(a.sq.batch, a.B, &st[3]) || !encode_map(&tq, a.q, 5, dims, st, box) || !encode_kv(&tk, a, a.k, a.sk, KEYS, &p.kh, &p.kb) ||
+        !encode_kv(&tv, a, a.v, a.sv, KEYS, &p.vh, &p.vb))
         return cudaErrorInvalidValue;
     int dev = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&dev);
