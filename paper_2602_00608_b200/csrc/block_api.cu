@@ -52,7 +52,8 @@ vd_status vd_op_cross_attention(const vd_xattn_desc* d, const void* q, const voi
     if (d->struct_size != sizeof(vd_xattn_desc)) return refuse(VD_ERR_INVALID_ARG, "vd_xattn_desc: struct_size mismatch");
     if (!is_dtype(d->dtype)) return refuse(VD_ERR_INVALID_ARG, "bad dtype");
     if (d->batch < 0 || d->q_len < 0 || d->kv_len < 0 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0 ||
-        d->head_dim < 1 || d->head_dim > 256 || !fits(d->batch, d->heads, d->q_len))
+        d->head_dim < 1 || d->head_dim > 256 || d->kv_len > 1 << 30 || !fits(d->batch, d->heads, d->q_len) ||
+        (int64_t)d->batch * d->heads * d->q_len > 1 << 30)
         return refuse(VD_ERR_INVALID_ARG, "bad attention sizes");
     if (d->impl < VD_XATTN_AUTO || d->impl > VD_XATTN_PLAIN) return refuse(VD_ERR_INVALID_ARG, "bad impl");
     if (!(d->scale > 0.f) || isinf(d->scale)) return refuse(VD_ERR_INVALID_ARG, "scale must be positive and finite");
@@ -68,7 +69,8 @@ vd_status vd_op_cross_attention(const vd_xattn_desc* d, const void* q, const voi
                 {d->o_batch, d->o_token, d->o_head}, d->scale};
     const int64_t rows = (int64_t)d->q_len * (d->heads / d->kv_heads);       // of a key head
     cudaError_t e;
-    if (d->impl == VD_XATTN_AUTO && rows <= 16 && xattn_rows_supported(a)) e = launch_xattn_rows(a, (cudaStream_t)cuda_stream);
+    if (d->impl == VD_XATTN_AUTO && rows <= (d->dtype == VD_BF16 ? 16 : 4) && xattn_rows_supported(a)) e = launch_xattn_rows(a, (cudaStream_t)cuda_stream);
+    else if (d->impl == VD_XATTN_AUTO && xattn_f32_supported(a)) e = launch_xattn_f32(a, (cudaStream_t)cuda_stream);
     else if (d->impl == VD_XATTN_AUTO && xattn_tc_supported(a)) e = launch_xattn_tc(a, (cudaStream_t)cuda_stream);
     else e = launch_xattn_plain(a, (cudaStream_t)cuda_stream);
     return done(e, "vd_op_cross_attention");

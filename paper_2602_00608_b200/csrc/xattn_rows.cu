@@ -6,35 +6,16 @@
 // The running maximum is a warp's, moved only when a score exceeds it by 2^8 (every lane's sums share it, so they add without
 // weights).  With more rows the arithmetic is what bounds this, and bf16 takes matrix instructions instead (below).  Warps meet in shared memory; where there are few heads, a cluster of up to eight CTAs divides the keys and meets in
 // distributed shared memory.  Fixed orders throughout: the same bits each time.
-#include <algorithm>
-#include <mutex>
-
 #include "block_ops.h"
-#include "conv_cluster.cuh"
-#include "tc_common.cuh"
-#include "tc_pair.cuh"
 #include "xattn_maps.h"
+#include "xattn_meet.cuh"
 
 namespace vd {
 namespace {
 
 using namespace tc;
+using namespace xa;
 
-constexpr int MAX_SPLITS = 8;
-constexpr float RESCALE_THRESHOLD = 8.0f;
-
-struct RowParams {
-    XAttnArgs a;
-    int g, groups;               // groups: of R rows, of a (batch item, key head)
-    int splits;
-    float scale_log2;
-};
-
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ uint4 ldg_stream(const void* p) {
     uint4 r;
     asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
@@ -57,7 +38,6 @@ template <> struct Vec<float> {
         f[1] = pack2(__uint_as_float(r.z), __uint_as_float(r.w));
     }
 };
-__device__ __forceinline__ void unpack2(unsigned long long v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
 
 // v[i] summed over the L lanes of a group; lane x of it is left with sum x / (L / N) in v[0]
 template <int N, int L> __device__ __forceinline__ float sum_scatter(float (&v)[N], int lane) {
@@ -80,36 +60,6 @@ template <int N, int L> __device__ __forceinline__ float sum_scatter(float (&v)[
     }
     return v[0];
 }
-
-// a CTA's row group, and what its rows are
-struct Work {
-    int b, kvh, row0, rows, len;
-    __device__ __forceinline__ int64_t at(const RowParams& p, const Strides& s, int r) const {
-        const int row = row0 + r, t = row / p.g, h = kvh * p.g + row - t * p.g;
-        return b * s.batch + t * s.token + h * s.head;
-    }
-};
-template <int R> __device__ __forceinline__ Work work_of(const RowParams& p) {
-    Work w;
-    const int64_t item = blockIdx.x / p.splits;
-    w.row0 = (int)(item % p.groups) * R;
-    w.kvh = (int)(item / p.groups % p.a.Hkv);
-    w.b = (int)(item / p.groups / p.a.Hkv);
-    w.rows = min(R, p.a.Tq * p.g - w.row0);
-    w.len = p.a.kv_lens ? min(max(p.a.kv_lens[w.b], 0), p.a.Tk) : p.a.Tk;
-    return w;
-}
-// shared memory: the warps' accumulators, the CTA's, and (maximum, sum) of either; `rows` rows of DM channels each
-template <int DM, int WARPS> struct Shared {
-    float* base;
-    int rows;
-    __device__ __forceinline__ Shared(float* b, int r) : base(b), rows(r) {}
-    __device__ __forceinline__ float* acc(int warp, int r) const { return base + (warp * rows + r) * DM; }
-    __device__ __forceinline__ float* out(int r) const { return acc(WARPS, r); }
-    __device__ __forceinline__ float2* ml(int warp, int r) const { return (float2*)acc(WARPS + 1, 0) + warp * rows + r; }
-    __device__ __forceinline__ float2* om(int r) const { return ml(WARPS, r); }
-};
-constexpr int shared_bytes(int warps, int rows, int dm) { return (warps + 1) * rows * (dm + 2) * 4; }
 
 // The warps' shares are in shared memory: added up and written, or left there for the cluster, whose CTAs each finish a part.
 template <typename T, int DM, int WARPS> __device__ __forceinline__ void meet(const RowParams& p, const Shared<DM, WARPS>& sh, const Work& w, int split, int tid) {
@@ -139,32 +89,7 @@ template <typename T, int DM, int WARPS> __device__ __forceinline__ void meet(co
             if (d == 0) *sh.om(r) = make_float2(m, sum);
         }
     }
-    if (p.splits == 1) return;
-    cluster_sync_all();                                      // every CTA's share is in its shared memory
-    for (int i = split * (WARPS * 32) + tid; i < w.rows * DM && tid < WARPS * 32; i += p.splits * WARPS * 32) {
-        const int r = i / DM, d = i % DM;
-        if (d >= a.D) continue;
-        float m[MAX_SPLITS], sum[MAX_SPLITS], o[MAX_SPLITS], top = -INFINITY;
-#pragma unroll
-        for (int c = 0; c < MAX_SPLITS; ++c)
-            if (c < p.splits) {
-                const uint32_t om = map_to_cta(smem_u32(sh.om(r)), (uint32_t)c), at = map_to_cta(smem_u32(sh.out(r) + d), (uint32_t)c);
-                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(m[c]), "=f"(sum[c]) : "r"(om) : "memory");
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o[c]) : "r"(at) : "memory");
-                top = fmaxf(top, m[c]);
-            }
-        const float ref = top == -INFINITY ? 0.f : top;
-        float total = 0.f, out = 0.f;
-#pragma unroll
-        for (int c = 0; c < MAX_SPLITS; ++c)
-            if (c < p.splits) {
-                const float f = ex2(m[c] - ref);
-                total = fmaf(f, sum[c], total);
-                out = fmaf(f, o[c], out);
-            }
-        ((T*)a.o)[w.at(p, a.so, r) + d] = (T)(w.len ? out / total : 0.f);
-    }
-    cluster_sync_all();                                      // nobody leaves while others read its memory
+    if (p.splits > 1) meet_cluster<T, DM, WARPS * 32>(p, sh.out(0), sh.om(0), w, split, tid);
 }
 
 template <typename T, int R, int U, int LPK, int NVL, int WARPS>
@@ -480,48 +405,6 @@ xattn_stream_kernel(const StreamParams sp, const __grid_constant__ CUtensorMap t
     meet<__nv_bfloat16, DP, STREAM_WARPS>(p, sh, w, split, tid);
 }
 
-// clusters of `splits` CTAs of KERNEL that the current device holds at once (0: none), asked once per device
-template <auto KERNEL> int clusters_held(int threads, int smem, int splits) {
-    static std::mutex mu;
-    static int known[cc::kMaxDevices][MAX_SPLITS] = {};      // 0: not asked, else the answer + 1
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= cc::kMaxDevices || cc::set_smem_limit<KERNEL>(smem) != cudaSuccess) {
-        cudaGetLastError();
-        return 0;
-    }
-    std::lock_guard<std::mutex> lock(mu);
-    int& k = known[dev][splits - 1];
-    if (k == 0) {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)splits);
-        cfg.blockDim = dim3((unsigned)threads);
-        cfg.dynamicSmemBytes = (size_t)smem;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)splits; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, (const void*)KERNEL, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
-        k = n + 1;
-    }
-    return k - 1;
-}
-
-// CTAs that share the keys of a group: the fewest waves of clusters x (rounds of a CTA + what a CTA costs besides, in rounds)
-template <auto KERNEL> RowParams plan_rows(const XAttnArgs& a, int threads, int rows, int smem, int round) {
-    RowParams p{a, a.H / a.Hkv, 0, 1, a.scale * 1.4426950408889634f};
-    p.groups = (int)(((int64_t)a.Tq * p.g + rows - 1) / rows);
-    const int64_t items = (int64_t)p.groups * a.Hkv * a.B;
-    double best = 0.0;
-    for (int n = 1; n <= MAX_SPLITS && (n == 1 || (n - 1) * round < a.Tk); ++n) {
-        const int held = clusters_held<KERNEL>(threads, smem, n);
-        if (held < 1) continue;
-        const double cost = (double)((items + held - 1) / held) * ((a.Tk + n * round - 1) / (n * round) + (n == 1 ? 2.0 : 3.0));
-        if (best == 0.0 || cost < best) { best = cost; p.splits = n; }
-    }
-    return p;
-}
 template <typename T, int R, int U, int LPK, int NVL> cudaError_t launch(const XAttnArgs& a, cudaStream_t s) {
     constexpr int W = 8, smem = shared_bytes(W, R, LPK * Vec<T>::E * NVL);
     const RowParams p = plan_rows<xattn_rows_kernel<T, R, U, LPK, NVL, W>>(a, W * 32, R, smem, 32 / LPK * U * W);

@@ -36,6 +36,7 @@ def test_struct_sizes_match_the_header_layout():
     dict(head_dim=0), dict(head_dim=257), dict(impl=9), dict(impl=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf), dict(scale=math.nan),
     dict(q_token=-1), dict(o_batch=-5), dict(o_token=0), dict(o_head=63), dict(o_batch=0), dict(o_batch=767),
     dict(batch=1 << 20, q_len=1 << 20), dict(batch=1 << 15, heads=1 << 14, kv_heads=1, q_len=4),
+    dict(kv_len=(1 << 30) + 1), dict(batch=1, heads=2, kv_heads=2, q_len=(1 << 29) + 1),
 ])
 def test_cross_attention_refuses(change):
     assert vd.lib().vd_op_cross_attention(ctypes.byref(xattn(**change)), P, P, P, None, P, None) == vd.VD_ERR_INVALID_ARG
