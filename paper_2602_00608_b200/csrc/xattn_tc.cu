@@ -27,6 +27,9 @@ using namespace tc;
 
 constexpr int ROWS = 128, KEYS = 128, CHUNK = 64;            // of a tile; channels of a 128-byte row
 constexpr int SOFTMAX_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, NUM_THREADS = 320;
+#ifndef POLY_EVERY
+#define POLY_EVERY 4
+#endif
 constexpr float RESCALE_THRESHOLD = 8.0f;                    // log2 units: accumulators may grow by 2^8
 
 template <int DP> struct Cfg {
@@ -98,6 +101,117 @@ __device__ __forceinline__ void umma_bf16_ts_on(uint32_t d_tmem, uint32_t a_tmem
         ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(on) : "memory");
 }
 
+// 32 scores into 32 numbers of P: 2^(score * scale - reference), their sums, bf16
+template <bool POLY>
+__device__ __forceinline__ void exp_chunk(const uint32_t (&r)[32], uint32_t t_p, unsigned long long sc, unsigned long long mr,
+                                          unsigned long long& sum, unsigned long long& sum_b) {
+    uint32_t pk[16];
+#pragma unroll
+    for (int q = 0; q < 32; q += 2) {
+        float e0, e1;
+        unpack2(fmaf2(pack2(__uint_as_float(r[q]), __uint_as_float(r[q + 1])), sc, mr), e0, e1);
+        if (POLY && (q / 2) % POLY_EVERY == POLY_EVERY - 1) {
+            ex2_poly2(e0, e1);
+        } else {
+            e0 = ex2(e0);
+            e1 = ex2(e1);
+        }
+        if (q & 2) sum_b = add2(sum_b, pack2(e0, e1));
+        else sum = add2(sum, pack2(e0, e1));
+        pk[q >> 1] = pack_bf16(e0, e1);
+    }
+    tmem_st16(t_p, pk);
+}
+__device__ __forceinline__ float max_of(const uint32_t (&r)[32], float m) {
+    float a = max3(__uint_as_float(r[0]), __uint_as_float(r[1]), m), b = max3(__uint_as_float(r[2]), __uint_as_float(r[3]), __uint_as_float(r[4]));
+#pragma unroll
+    for (int q = 5; q < 29; q += 4) {
+        a = max3(a, __uint_as_float(r[q]), __uint_as_float(r[q + 1]));
+        b = max3(b, __uint_as_float(r[q + 2]), __uint_as_float(r[q + 3]));
+    }
+    a = max3(a, __uint_as_float(r[29]), __uint_as_float(r[30]));
+    return max3(a, b, __uint_as_float(r[31]));
+}
+// Lazy rescale of a row: keep the old reference unless the maximum grew by more than the threshold.
+template <int DP>
+__device__ __forceinline__ void move_reference(float top, uint32_t t_o, bool rescale, float& m_ref, unsigned long long& sum, unsigned long long& sum_b) {
+    const bool grow = top > m_ref + RESCALE_THRESHOLD;
+    if (!__any_sync(0xffffffffu, grow)) return;
+    float factor = 1.f;
+    if (grow) {
+        factor = ex2(m_ref - top);                           // 0 at the first tile
+        m_ref = top;
+    }
+    sum = fmaf2(sum, pack2(factor, factor), 0ull);
+    sum_b = fmaf2(sum_b, pack2(factor, factor), 0ull);
+    if (rescale) {                                           // (the scores were issued behind the last product into O: it is complete)
+#pragma unroll 1
+        for (uint32_t c = 0; c < (uint32_t)DP; c += 16u) {
+            uint32_t o[16];
+            tmem_ld16(t_o + c, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int q = 0; q < 16; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * factor);
+            tmem_st16(t_o + c, o);
+        }
+    }
+}
+// One row's tile of scores: maximum, rescale of the row's output, exponentials into P, which lies over the scores (32 of them make
+// 16 columns of P, so those still to be read are not touched).  Returns the tile's maximum, NaN if a score is.  Two chunks of 32 stay in
+// registers from the maximum to the exponentials, the others are read again: 128 at once leave ptxas no room.
+template <int DP>
+__device__ __forceinline__ float softmax_full(float scale_log2, uint32_t t_s, uint32_t t_o, bool rescale, float& m_ref, unsigned long long& sum, unsigned long long& sum_b) {
+    uint32_t a[32], b[32];
+    tmem_ld32(t_s + 64u, a);
+    tmem_ld32(t_s + 96u, b);
+    tmem_ld_wait();
+    float tmax = max_of(b, max_of(a, -INFINITY));
+    tmem_ld32(t_s, a);
+    tmem_ld32(t_s + 32u, b);
+    tmem_ld_wait();
+    tmax = max_of(b, max_of(a, tmax));
+    move_reference<DP>(tmax * scale_log2, t_o, rescale, m_ref, sum, sum_b);
+    const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+    const unsigned long long sc = pack2(scale_log2, scale_log2), mr = pack2(-ref, -ref);
+    exp_chunk<true>(a, t_s, sc, mr, sum, sum_b);
+    tmem_ld32(t_s + 64u, a);
+    exp_chunk<true>(b, t_s + 16u, sc, mr, sum, sum_b);
+    tmem_ld32(t_s + 96u, b);
+    tmem_ld_wait();
+    exp_chunk<true>(a, t_s + 32u, sc, mr, sum, sum_b);
+    exp_chunk<true>(b, t_s + 48u, sc, mr, sum, sum_b);
+    return tmax;
+}
+// The same where only the first `valid` keys of the tile count: the others leave before the maximum.
+template <int DP>
+__device__ __forceinline__ float softmax_part(float scale_log2, uint32_t t_s, uint32_t t_o, int valid, bool rescale, float& m_ref,
+                                              unsigned long long& sum, unsigned long long& sum_b) {
+    uint32_t r[32];
+    float tmax = -INFINITY;
+#pragma unroll 1
+    for (int c = 0; c < valid; c += 32) {
+        tmem_ld32(t_s + (uint32_t)c, r);
+        tmem_ld_wait();
+#pragma unroll
+        for (int q = 0; q < 32; ++q)
+            if (c + q >= valid) r[q] = __float_as_uint(-INFINITY);
+        tmax = max_of(r, tmax);
+    }
+    move_reference<DP>(tmax * scale_log2, t_o, rescale, m_ref, sum, sum_b);
+    const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+    const unsigned long long sc = pack2(scale_log2, scale_log2), mr = pack2(-ref, -ref);
+#pragma unroll 1
+    for (int c = 0; c < valid; c += 32) {
+        tmem_ld32(t_s + (uint32_t)c, r);
+        tmem_ld_wait();
+#pragma unroll
+        for (int q = 0; q < 32; ++q)
+            if (c + q >= valid) r[q] = __float_as_uint(-INFINITY);
+        exp_chunk<false>(r, t_s + (uint32_t)(c >> 1), sc, mr, sum, sum_b);
+    }
+    return tmax;
+}
+
 struct Item { int b, kvh, t0, streams, len, tiles; };
 __device__ __forceinline__ Item item_of(const Params& a, int64_t i) {
     Item r;
@@ -150,88 +264,15 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
             const Item it = item_of(a, i);
             if (s >= it.streams) continue;
             float m_ref = -INFINITY;
-            unsigned long long l2 = 0, l2b = 0;
-            float l = 0.f;
+            unsigned long long sum = 0, sum_b = 0;           // of even and odd pairs of keys
+            bool bad = false;
             for (int j = 0; j < it.tiles; ++j, ++n_s) {
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->s_full[s]), n_s & 1, abort_flag)) && ok;
                 tc_fence_after();
                 const int valid = it.len - j * KEYS;
-                uint32_t r[4][32];
-                float tmax;
-                if (valid >= KEYS) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(t_s + (uint32_t)c * 32u, r[c]);
-                    tmem_ld_wait();
-                    float m[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        m[c] = max3(__uint_as_float(r[c][0]), __uint_as_float(r[c][1]), __uint_as_float(r[c][2]));
-#pragma unroll
-                        for (int q = 3; q < 31; q += 2) m[c] = max3(m[c], __uint_as_float(r[c][q]), __uint_as_float(r[c][q + 1]));
-                        m[c] = max3(m[c], __uint_as_float(r[c][31]), __uint_as_float(r[c][31]));
-                    }
-                    tmax = max3(max3(m[0], m[1], m[2]), m[3], m[3]);
-                } else {                                     // keys that do not count leave before the maximum
-                    tmax = -INFINITY;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        if (c * 32 >= valid) break;
-                        tmem_ld32(t_s + (uint32_t)c * 32u, r[c]);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int q = 0; q < 32; ++q) {
-                            if (c * 32 + q >= valid) r[c][q] = __float_as_uint(-INFINITY);
-                            tmax = max3(tmax, __uint_as_float(r[c][q]), __uint_as_float(r[c][q]));
-                        }
-                    }
-                }
-                tmax *= a.scale_log2;
-                // lazy rescale: keep the old reference unless the maximum grew by more than the threshold
-                const bool grow = tmax > m_ref + RESCALE_THRESHOLD;
-                if (__any_sync(0xffffffffu, grow)) {
-                    float factor = 1.f;
-                    if (grow) {
-                        factor = ex2(m_ref - tmax);          // 0 at the first tile
-                        m_ref = tmax;
-                    }
-                    l *= factor;
-                    l2 = fmaf2(l2, pack2(factor, factor), 0ull);
-                    l2b = fmaf2(l2b, pack2(factor, factor), 0ull);
-                    if (j > 0) {                             // (the scores were issued behind the last product into O: it is complete)
-#pragma unroll 1
-                        for (uint32_t c = 0; c < (uint32_t)DP; c += 16u) {
-                            uint32_t o[16];
-                            tmem_ld16(t_o + c, o);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int q = 0; q < 16; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * factor);
-                            tmem_st16(t_o + c, o);
-                        }
-                    }
-                }
-                const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-                const unsigned long long sc = pack2(a.scale_log2, a.scale_log2), mr = pack2(-ref, -ref);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    if (c * 32 >= valid) break;
-                    uint32_t pk[16];
-#pragma unroll
-                    for (int q = 0; q < 32; q += 2) {
-                        float e0, e1;
-                        unpack2(fmaf2(pack2(__uint_as_float(r[c][q]), __uint_as_float(r[c][q + 1])), sc, mr), e0, e1);
-                        if ((q & 7) == 6 && valid >= KEYS) {         // a quarter
-                            ex2_poly2(e0, e1);
-                        } else {
-                            e0 = ex2(e0);
-                            e1 = ex2(e1);
-                        }
-                        if (q & 2) l2b = add2(l2b, pack2(e0, e1));
-                        else l2 = add2(l2, pack2(e0, e1));
-                        pk[q >> 1] = pack_bf16(e0, e1);
-                    }
-                    tmem_st16(t_s + (uint32_t)c * 16u, pk);
-                }
-                if (!(tmax < INFINITY)) l = __int_as_float(0x7fffffff);      // a NaN or an infinity among the scores
+                const float tmax = valid >= KEYS ? softmax_full<DP>(a.scale_log2, t_s, t_o, j > 0, m_ref, sum, sum_b)
+                                                 : softmax_part<DP>(a.scale_log2, t_s, t_o, valid, j > 0, m_ref, sum, sum_b);
+                bad = bad || !(tmax < INFINITY);             // a NaN or an infinity among the scores
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
@@ -242,8 +283,7 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                 tc_fence_after();
                 ++n_o;
             }
-            l += sum2(add2(l2, l2b));
-            const float inv = it.tiles == 0 ? 0.f : ok ? 1.f / l : __int_as_float(0x7fffffff);
+            const float inv = it.tiles == 0 ? 0.f : ok && !bad ? 1.f / sum2(add2(sum, sum_b)) : __int_as_float(0x7fffffff);
             const int t = it.t0 + s * a.nt + tt;
             const bool inside = tt < a.nt && t < a.Tq;
             __nv_bfloat16* o = (__nv_bfloat16*)a.o + it.b * a.o_batch + t * a.o_token + (it.kvh * a.g + hg) * a.o_head;
