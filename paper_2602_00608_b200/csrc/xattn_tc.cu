@@ -39,7 +39,7 @@ template <int DP> struct Cfg {
     static constexpr int SMEM = (Q_BUFS * 2 + STAGES) * TILE_BYTES + 512 + 1024;
 };
 struct Bars {
-    uint64_t q_full[2], q_empty[2], full[6], empty[6], s_full[2], p_full[2], o_full[2], drained;
+    uint64_t q_full[2], q_empty[2], full[6], empty[6], s_full[2], p_half[2], p_full[2], o_full[2], drained;
     uint32_t tmem_base, abort_flag;
 };
 static_assert(sizeof(Bars) <= 512 && Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448, "shared memory of one CTA");
@@ -132,18 +132,35 @@ __device__ __forceinline__ float max_of(const uint32_t (&r)[32], float m) {
     a = max3(a, __uint_as_float(r[29]), __uint_as_float(r[30]));
     return max3(a, b, __uint_as_float(r[31]));
 }
-// Lazy rescale of a row: keep the old reference unless the maximum grew by more than the threshold.
+// A row's reference, an integer that its exponentials are relative to: it stays unless a score exceeds it by more than the threshold, and
+// moves by a power of two, so that what has been summed (O, the sums, P as far as it is written) is rescaled without rounding.
 template <int DP>
-__device__ __forceinline__ void move_reference(float top, uint32_t t_o, bool rescale, float& m_ref, unsigned long long& sum, unsigned long long& sum_b) {
+__device__ __forceinline__ void move_reference(float top, uint32_t t_p, uint32_t p_cols, uint32_t t_o, bool rescale, float& m_ref,
+                                               unsigned long long& sum, unsigned long long& sum_b) {
     const bool grow = top > m_ref + RESCALE_THRESHOLD;
     if (!__any_sync(0xffffffffu, grow)) return;
     float factor = 1.f;
     if (grow) {
-        factor = ex2(m_ref - top);                           // 0 at the first tile
-        m_ref = top;
+        const float to = ceilf(top), by = to - m_ref;        // (infinite at the first tile)
+        factor = by < 127.f ? __int_as_float((127 - (int)by) << 23) : 0.f;
+        m_ref = to;
     }
     sum = fmaf2(sum, pack2(factor, factor), 0ull);
     sum_b = fmaf2(sum_b, pack2(factor, factor), 0ull);
+    if (p_cols) tmem_st_wait();
+#pragma unroll 1
+    for (uint32_t c = 0; c < p_cols; c += 16u) {
+        uint32_t v[16];
+        tmem_ld16(t_p + c, v);
+        tmem_ld_wait();
+        const __nv_bfloat162 f = __floats2bfloat162_rn(factor, factor);
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v[q]), f);
+            v[q] = *reinterpret_cast<const uint32_t*>(&x);
+        }
+        tmem_st16(t_p + c, v);
+    }
     if (rescale) {                                           // (the scores were issued behind the last product into O: it is complete)
 #pragma unroll 1
         for (uint32_t c = 0; c < (uint32_t)DP; c += 16u) {
@@ -156,31 +173,40 @@ __device__ __forceinline__ void move_reference(float top, uint32_t t_o, bool res
         }
     }
 }
-// One row's tile of scores: maximum, rescale of the row's output, exponentials into P, which lies over the scores (32 of them make
-// 16 columns of P, so those still to be read are not touched).  Returns the tile's maximum, NaN if a score is.  Two chunks of 32 stay in
-// registers from the maximum to the exponentials, the others are read again: 128 at once leave ptxas no room.
+// P as far as it is written is there for the tensor core
+__device__ __forceinline__ void hand_over(uint64_t* bar, int lane) {
+    tmem_st_wait();
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(bar));
+}
+// One row's tile of scores: exponentials into P, which lies over the scores (32 of them make 16 columns of P, so those still to be read
+// are not touched).  The maximum is only needed to see that the reference may stay, so it is taken half a tile at a time in front of
+// the exponentials, and the first half of P goes to the tensor core while the second one is made.  Returns the tile's maximum, NaN if
+// a score is.
 template <int DP>
-__device__ __forceinline__ float softmax_full(float scale_log2, uint32_t t_s, uint32_t t_o, bool rescale, float& m_ref, unsigned long long& sum, unsigned long long& sum_b) {
-    uint32_t a[32], b[32];
-    tmem_ld32(t_s + 64u, a);
-    tmem_ld32(t_s + 96u, b);
-    tmem_ld_wait();
-    float tmax = max_of(b, max_of(a, -INFINITY));
+__device__ __forceinline__ float softmax_full(float scale_log2, uint32_t t_s, uint32_t t_o, bool rescale, float& m_ref, unsigned long long& sum,
+                                              unsigned long long& sum_b, uint64_t* half, int lane) {
+    uint32_t a[32], b[32], c[32];
     tmem_ld32(t_s, a);
     tmem_ld32(t_s + 32u, b);
+    tmem_ld32(t_s + 64u, c);
     tmem_ld_wait();
-    tmax = max_of(b, max_of(a, tmax));
-    move_reference<DP>(tmax * scale_log2, t_o, rescale, m_ref, sum, sum_b);
-    const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-    const unsigned long long sc = pack2(scale_log2, scale_log2), mr = pack2(-ref, -ref);
-    exp_chunk<true>(a, t_s, sc, mr, sum, sum_b);
-    tmem_ld32(t_s + 64u, a);
-    exp_chunk<true>(b, t_s + 16u, sc, mr, sum, sum_b);
-    tmem_ld32(t_s + 96u, b);
+    const float t0 = max_of(b, max_of(a, -INFINITY));
+    move_reference<DP>(t0 * scale_log2, t_s, 0u, t_o, rescale, m_ref, sum, sum_b);
+    const unsigned long long sc = pack2(scale_log2, scale_log2);
+    float ref = m_ref == -INFINITY ? 0.f : m_ref;
+    exp_chunk<true>(a, t_s, sc, pack2(-ref, -ref), sum, sum_b);
+    tmem_ld32(t_s + 96u, a);
+    exp_chunk<true>(b, t_s + 16u, sc, pack2(-ref, -ref), sum, sum_b);
     tmem_ld_wait();
-    exp_chunk<true>(a, t_s + 32u, sc, mr, sum, sum_b);
-    exp_chunk<true>(b, t_s + 48u, sc, mr, sum, sum_b);
-    return tmax;
+    const float t1 = max_of(a, max_of(c, t0));
+    move_reference<DP>(t1 * scale_log2, t_s, 32u, t_o, rescale, m_ref, sum, sum_b);
+    hand_over(half, lane);
+    ref = m_ref == -INFINITY ? 0.f : m_ref;
+    exp_chunk<true>(c, t_s + 32u, sc, pack2(-ref, -ref), sum, sum_b);
+    exp_chunk<true>(a, t_s + 48u, sc, pack2(-ref, -ref), sum, sum_b);
+    return t1;
 }
 // The same where only the first `valid` keys of the tile count: the others leave before the maximum.
 template <int DP>
@@ -197,7 +223,7 @@ __device__ __forceinline__ float softmax_part(float scale_log2, uint32_t t_s, ui
             if (c + q >= valid) r[q] = __float_as_uint(-INFINITY);
         tmax = max_of(r, tmax);
     }
-    move_reference<DP>(tmax * scale_log2, t_o, rescale, m_ref, sum, sum_b);
+    move_reference<DP>(tmax * scale_log2, t_s, 0u, t_o, rescale, m_ref, sum, sum_b);
     const float ref = m_ref == -INFINITY ? 0.f : m_ref;
     const unsigned long long sc = pack2(scale_log2, scale_log2), mr = pack2(-ref, -ref);
 #pragma unroll 1
@@ -239,7 +265,7 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&bars->q_full[i]), 1); mbar_init(smem_u32(&bars->q_empty[i]), 1);
-            mbar_init(smem_u32(&bars->s_full[i]), 1); mbar_init(smem_u32(&bars->p_full[i]), SOFTMAX_WARPS / 2); mbar_init(smem_u32(&bars->o_full[i]), 1);
+            mbar_init(smem_u32(&bars->s_full[i]), 1); mbar_init(smem_u32(&bars->p_half[i]), SOFTMAX_WARPS / 2); mbar_init(smem_u32(&bars->p_full[i]), SOFTMAX_WARPS / 2); mbar_init(smem_u32(&bars->o_full[i]), 1);
         }
         for (int i = 0; i < C::STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), 1); }
         mbar_init(smem_u32(&bars->drained), 1);
@@ -270,13 +296,11 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->s_full[s]), n_s & 1, abort_flag)) && ok;
                 tc_fence_after();
                 const int valid = it.len - j * KEYS;
-                const float tmax = valid >= KEYS ? softmax_full<DP>(a.scale_log2, t_s, t_o, j > 0, m_ref, sum, sum_b)
+                const float tmax = valid >= KEYS ? softmax_full<DP>(a.scale_log2, t_s, t_o, j > 0, m_ref, sum, sum_b, &bars->p_half[s], lane)
                                                  : softmax_part<DP>(a.scale_log2, t_s, t_o, valid, j > 0, m_ref, sum, sum_b);
                 bad = bad || !(tmax < INFINITY);             // a NaN or an infinity among the scores
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bars->p_full[s]));
+                if (valid < KEYS) hand_over(&bars->p_half[s], lane);
+                hand_over(&bars->p_full[s], lane);
             }
             if (it.tiles) {
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->o_full[s]), n_o & 1, abort_flag)) && ok;
@@ -378,11 +402,12 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
             commit(&bars->s_full[s]);
             __syncwarp();
         };
-        auto issue_pv = [&](int s, uint32_t stage, int steps, bool first) {
+        auto issue_pv = [&](int s, uint32_t stage, int from, int steps, bool first) {
             const uint32_t v_lo = desc_lo(smem_u32(smem_st + stage * C::TILE_BYTES)) | (((KEYS * 128u) >> 4) << 16);
             const uint32_t d = tmem + 256u + (uint32_t)(s * DP), p = tmem + (uint32_t)s * 128u;
 #pragma unroll
-            for (int k = 0; k < KEYS / 16; ++k) {
+            for (int i = 0; i < KEYS / 32; ++i) {
+                const int k = from + i;
                 if (k >= steps) break;
                 umma_bf16_ts_on(d, p + (uint32_t)k * 8u, v_lo + (uint32_t)k * (2048u >> 4), hi, idesc_pv, first && k == 0 ? 0u : 1u, on);
             }
@@ -413,9 +438,11 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                     __syncwarp();
                 }
                 for (int s = 0; s < it.streams; ++s) {
+                    wait_on(&bars->p_half[s], n_p[s] & 1);
+                    issue_pv(s, v_st, 0, steps, j == 0);
                     wait_on(&bars->p_full[s], n_p[s] & 1);
+                    issue_pv(s, v_st, KEYS / 32, steps, false);
                     ++n_p[s];
-                    issue_pv(s, v_st, steps, j == 0);
                     if (s + 1 == it.streams) commit(&bars->empty[v_st]);
                     if (last) {
                         commit(&bars->o_full[s]);
