@@ -26,20 +26,26 @@ namespace {
 using namespace tc;
 
 constexpr int ROWS = 128, KEYS = 128, CHUNK = 64;            // of a tile; channels of a 128-byte row
-constexpr int SOFTMAX_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, NUM_THREADS = 320;
-#ifndef POLY_EVERY
-#define POLY_EVERY 4
-#endif
+constexpr int HALF = KEYS / 2;                               // keys of P that go to the tensor core at a time
+constexpr int SOFTMAX_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, NUM_THREADS = 352;     // MMA_WARP + s issues for tile s
 constexpr float RESCALE_THRESHOLD = 8.0f;                    // log2 units: accumulators may grow by 2^8
 
 template <int DP> struct Cfg {
     static constexpr int CHUNKS = DP / CHUNK;
     static constexpr int TILE_BYTES = ROWS * DP * 2;         // of Q (a tile), K or V
     static constexpr int STAGES = DP == 128 ? 3 : 6, Q_BUFS = 2;
+    // Tensor memory has room for a P of its own beside the scores where O takes 64 columns: the next scores then do not wait for the
+    // products of P.  Columns of tile s: S at 128 s, O at 256 + DP s, P at P_COL + P_STEP s.
+    static constexpr bool APART = DP == 64;
+    static constexpr uint32_t P_COL = APART ? 384 : 0, P_STEP = APART ? 64 : 128;
+    // every so many pairs of exponentials one on the FMA pipes; 0: none.  (They take five instructions for one, and where the products are
+    // short the issue slots are what is short.)
+    static constexpr int POLY = APART ? 0 : 8;
+    static constexpr int MMA_WARPS = APART ? 2 : 1;
     static constexpr int SMEM = (Q_BUFS * 2 + STAGES) * TILE_BYTES + 512 + 1024;
 };
 struct Bars {
-    uint64_t q_full[2], q_empty[2], full[6], empty[6], s_full[2], p_half[2], p_full[2], o_full[2], drained;
+    uint64_t q_full[2], q_empty[2], full[6], empty[6], s_full[2], s_free[2], p_part[2][2], pv_done[2], o_full[2], drained[2];
     uint32_t tmem_base, abort_flag;
 };
 static_assert(sizeof(Bars) <= 512 && Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448, "shared memory of one CTA");
@@ -50,7 +56,8 @@ struct Params {
     int Tq, Tk, Hkv, g, D, nt;       // nt: tokens of a tile
     int q_items;                     // items of a (batch item, key head)
     int kb, vb, kh, vh;              // 0: the batch (head) coordinate of k or v stays 0
-    int64_t items, o_batch, o_token, o_head;
+    uint32_t items;
+    int64_t o_batch, o_token, o_head;
     float scale_log2;
 };
 
@@ -101,8 +108,8 @@ __device__ __forceinline__ void umma_bf16_ts_on(uint32_t d_tmem, uint32_t a_tmem
         ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(on) : "memory");
 }
 
-// 32 scores into 32 numbers of P: 2^(score * scale - reference), their sums, bf16
-template <bool POLY>
+// 32 scores into 32 numbers of P: 2^(score * scale - reference), their sums, bf16; every POLY-th pair on the FMA pipes
+template <int POLY>
 __device__ __forceinline__ void exp_chunk(const uint32_t (&r)[32], uint32_t t_p, unsigned long long sc, unsigned long long mr,
                                           unsigned long long& sum, unsigned long long& sum_b) {
     uint32_t pk[16];
@@ -110,7 +117,7 @@ __device__ __forceinline__ void exp_chunk(const uint32_t (&r)[32], uint32_t t_p,
     for (int q = 0; q < 32; q += 2) {
         float e0, e1;
         unpack2(fmaf2(pack2(__uint_as_float(r[q]), __uint_as_float(r[q + 1])), sc, mr), e0, e1);
-        if (POLY && (q / 2) % POLY_EVERY == POLY_EVERY - 1) {
+        if (POLY && (q / 2) % (POLY ? POLY : 1) == POLY - 1) {
             ex2_poly2(e0, e1);
         } else {
             e0 = ex2(e0);
@@ -132,124 +139,160 @@ __device__ __forceinline__ float max_of(const uint32_t (&r)[32], float m) {
     a = max3(a, __uint_as_float(r[29]), __uint_as_float(r[30]));
     return max3(a, b, __uint_as_float(r[31]));
 }
-// A row's reference, an integer that its exponentials are relative to: it stays unless a score exceeds it by more than the threshold, and
-// moves by a power of two, so that what has been summed (O, the sums, P as far as it is written) is rescaled without rounding.
-template <int DP>
-__device__ __forceinline__ void move_reference(float top, uint32_t t_p, uint32_t p_cols, uint32_t t_o, bool rescale, float& m_ref,
-                                               unsigned long long& sum, unsigned long long& sum_b) {
-    const bool grow = top > m_ref + RESCALE_THRESHOLD;
-    if (!__any_sync(0xffffffffu, grow)) return;
-    float factor = 1.f;
-    if (grow) {
-        const float to = ceilf(top), by = to - m_ref;        // (infinite at the first tile)
-        factor = by < 127.f ? __int_as_float((127 - (int)by) << 23) : 0.f;
-        m_ref = to;
-    }
-    sum = fmaf2(sum, pack2(factor, factor), 0ull);
-    sum_b = fmaf2(sum_b, pack2(factor, factor), 0ull);
-    if (p_cols) tmem_st_wait();
-#pragma unroll 1
-    for (uint32_t c = 0; c < p_cols; c += 16u) {
-        uint32_t v[16];
-        tmem_ld16(t_p + c, v);
-        tmem_ld_wait();
-        const __nv_bfloat162 f = __floats2bfloat162_rn(factor, factor);
-#pragma unroll
-        for (int q = 0; q < 16; ++q) {
-            const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v[q]), f);
-            v[q] = *reinterpret_cast<const uint32_t*>(&x);
-        }
-        tmem_st16(t_p + c, v);
-    }
-    if (rescale) {                                           // (the scores were issued behind the last product into O: it is complete)
-#pragma unroll 1
-        for (uint32_t c = 0; c < (uint32_t)DP; c += 16u) {
-            uint32_t o[16];
-            tmem_ld16(t_o + c, o);
-            tmem_ld_wait();
-#pragma unroll
-            for (int q = 0; q < 16; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * factor);
-            tmem_st16(t_o + c, o);
-        }
-    }
-}
-// P as far as it is written is there for the tensor core
+// P as far as it is written (scores as far as they are read) is the tensor core's
 __device__ __forceinline__ void hand_over(uint64_t* bar, int lane) {
-    tmem_st_wait();
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(bar));
 }
-// One row's tile of scores: exponentials into P, which lies over the scores (32 of them make 16 columns of P, so those still to be read
-// are not touched).  The maximum is only needed to see that the reference may stay, so it is taken half a tile at a time in front of
-// the exponentials, and the first half of P goes to the tensor core while the second one is made.  Returns the tile's maximum, NaN if
-// a score is.
-template <int DP>
-__device__ __forceinline__ float softmax_full(float scale_log2, uint32_t t_s, uint32_t t_o, bool rescale, float& m_ref, unsigned long long& sum,
-                                              unsigned long long& sum_b, uint64_t* half, int lane) {
-    uint32_t a[32], b[32], c[32];
-    tmem_ld32(t_s, a);
-    tmem_ld32(t_s + 32u, b);
-    tmem_ld32(t_s + 64u, c);
-    tmem_ld_wait();
-    const float t0 = max_of(b, max_of(a, -INFINITY));
-    move_reference<DP>(t0 * scale_log2, t_s, 0u, t_o, rescale, m_ref, sum, sum_b);
-    const unsigned long long sc = pack2(scale_log2, scale_log2);
-    float ref = m_ref == -INFINITY ? 0.f : m_ref;
-    exp_chunk<true>(a, t_s, sc, pack2(-ref, -ref), sum, sum_b);
-    tmem_ld32(t_s + 96u, a);
-    exp_chunk<true>(b, t_s + 16u, sc, pack2(-ref, -ref), sum, sum_b);
-    tmem_ld_wait();
-    const float t1 = max_of(a, max_of(c, t0));
-    move_reference<DP>(t1 * scale_log2, t_s, 32u, t_o, rescale, m_ref, sum, sum_b);
-    hand_over(half, lane);
-    ref = m_ref == -INFINITY ? 0.f : m_ref;
-    exp_chunk<true>(c, t_s + 32u, sc, pack2(-ref, -ref), sum, sum_b);
-    exp_chunk<true>(a, t_s + 48u, sc, pack2(-ref, -ref), sum, sum_b);
-    return t1;
-}
-// The same where only the first `valid` keys of the tile count: the others leave before the maximum.
-template <int DP>
-__device__ __forceinline__ float softmax_part(float scale_log2, uint32_t t_s, uint32_t t_o, int valid, bool rescale, float& m_ref,
-                                              unsigned long long& sum, unsigned long long& sum_b) {
-    uint32_t r[32];
-    float tmax = -INFINITY;
-#pragma unroll 1
-    for (int c = 0; c < valid; c += 32) {
-        tmem_ld32(t_s + (uint32_t)c, r);
-        tmem_ld_wait();
-#pragma unroll
-        for (int q = 0; q < 32; ++q)
-            if (c + q >= valid) r[q] = __float_as_uint(-INFINITY);
-        tmax = max_of(r, tmax);
-    }
-    move_reference<DP>(tmax * scale_log2, t_s, 0u, t_o, rescale, m_ref, sum, sum_b);
-    const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-    const unsigned long long sc = pack2(scale_log2, scale_log2), mr = pack2(-ref, -ref);
-#pragma unroll 1
-    for (int c = 0; c < valid; c += 32) {
-        tmem_ld32(t_s + (uint32_t)c, r);
-        tmem_ld_wait();
-#pragma unroll
-        for (int q = 0; q < 32; ++q)
-            if (c + q >= valid) r[q] = __float_as_uint(-INFINITY);
-        exp_chunk<false>(r, t_s + (uint32_t)(c >> 1), sc, mr, sum, sum_b);
-    }
-    return tmax;
-}
+// One row's tile of scores: exponentials into P.  Where P lies over the scores, 32 of them make 16 columns of it, so those still to be read
+// are not touched.
+template <int DP> struct Tile {
+    float scale_log2;
+    uint32_t t_s, t_p, t_o;
+    bool rescale;                // O holds something
+    uint64_t* s_free;            // to be told when the scores have been read, or null
+    uint64_t* pv_done;           // to be waited for before P is written or O rescaled, or null
+    uint32_t pv_parity;
+    volatile uint32_t* abort_flag;
+    int lane;
+    float m_ref;
+    unsigned long long sum, sum_b;       // of even and odd pairs of keys
+    bool ok = true;
 
-struct Item { int b, kvh, t0, streams, len, tiles; };
-__device__ __forceinline__ Item item_of(const Params& a, int64_t i) {
-    Item r;
-    const int qt = (int)(i % a.q_items), bh = (int)(i / a.q_items);
-    r.b = bh / a.Hkv;
-    r.kvh = bh - r.b * a.Hkv;
-    r.t0 = qt * 2 * a.nt;
-    r.streams = r.t0 + a.nt < a.Tq ? 2 : 1;
-    r.len = a.lens ? min(max(a.lens[r.b], 0), a.Tk) : a.Tk;
-    r.tiles = (r.len + KEYS - 1) / KEYS;
-    return r;
-}
+    // The reference is an integer that the exponentials are relative to: it stays unless a score exceeds it by more than the threshold, and
+    // moves by a power of two, so that what has been summed (O, the sums, P as far as it is written) is rescaled without rounding.
+    __device__ __forceinline__ void move_reference(float top, uint32_t p_cols) {
+        const bool grow = top > m_ref + RESCALE_THRESHOLD;
+        if (!__any_sync(0xffffffffu, grow)) return;
+        float factor = 1.f;
+        if (grow) {
+            const float to = ceilf(top), by = to - m_ref;    // (infinite at the first tile)
+            factor = by < 127.f ? __int_as_float((127 - (int)by) << 23) : 0.f;
+            m_ref = to;
+        }
+        sum = fmaf2(sum, pack2(factor, factor), 0ull);
+        sum_b = fmaf2(sum_b, pack2(factor, factor), 0ull);
+        if (p_cols) tmem_st_wait();
+#pragma unroll 1
+        for (uint32_t c = 0; c < p_cols; c += 16u) {
+            uint32_t v[16];
+            tmem_ld16(t_p + c, v);
+            tmem_ld_wait();
+            const __nv_bfloat162 f = __floats2bfloat162_rn(factor, factor);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v[q]), f);
+                v[q] = *reinterpret_cast<const uint32_t*>(&x);
+            }
+            tmem_st16(t_p + c, v);
+        }
+        if (rescale) {
+#pragma unroll 1
+            for (uint32_t c = 0; c < (uint32_t)DP; c += 16u) {
+                uint32_t o[16];
+                tmem_ld16(t_o + c, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int q = 0; q < 16; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * factor);
+                tmem_st16(t_o + c, o);
+            }
+        }
+    }
+    __device__ __forceinline__ unsigned long long minus_ref() const {
+        const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+        return pack2(-ref, -ref);
+    }
+    // (Without a barrier to wait for: the scores were issued behind the last product into O and of P, which is complete then.)
+    __device__ __forceinline__ void wait_pv() {
+        if (!pv_done) return;
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(pv_done), pv_parity, abort_flag)) && ok;
+        tc_fence_after();
+    }
+    // All 128 keys count.  The maximum is only needed to see that the reference may stay, so it is taken half a tile at a time in front
+    // of the exponentials, and the first half of P goes to the tensor core while the second one is made.  Returns the tile's maximum, NaN if
+    // a score is.
+    __device__ __forceinline__ float full(uint64_t* first_half) {
+        constexpr int POLY = Cfg<DP>::POLY;
+        uint32_t a[32], b[32], c[32];
+        tmem_ld32(t_s, a);
+        tmem_ld32(t_s + 32u, b);
+        tmem_ld32(t_s + 64u, c);
+        tmem_ld_wait();
+        const float t0 = max_of(b, max_of(a, -INFINITY));
+        wait_pv();
+        move_reference(t0 * scale_log2, 0u);
+        const unsigned long long sc = pack2(scale_log2, scale_log2);
+        unsigned long long mr = minus_ref();
+        exp_chunk<POLY>(a, t_p, sc, mr, sum, sum_b);
+        tmem_ld32(t_s + 96u, a);
+        exp_chunk<POLY>(b, t_p + 16u, sc, mr, sum, sum_b);
+        tmem_ld_wait();
+        if (s_free) hand_over(s_free, lane);
+        const float t1 = max_of(a, max_of(c, t0));
+        move_reference(t1 * scale_log2, 32u);
+        tmem_st_wait();
+        hand_over(first_half, lane);
+        mr = minus_ref();
+        exp_chunk<POLY>(c, t_p + 32u, sc, mr, sum, sum_b);
+        exp_chunk<POLY>(a, t_p + 48u, sc, mr, sum, sum_b);
+        return t1;
+    }
+    // Only the first `valid` keys count: the others leave before the maximum.  (The code of full() with masks spills in both.)
+    __device__ __forceinline__ float part(int valid, uint64_t* first_half) {
+        uint32_t r[32];
+        float top = -INFINITY;
+#pragma unroll 1
+        for (int c = 0; c < valid; c += 32) {
+            tmem_ld32(t_s + (uint32_t)c, r);
+            tmem_ld_wait();
+            mask(r, valid - c);
+            top = max_of(r, top);
+        }
+        wait_pv();
+        move_reference(top * scale_log2, 0u);
+        const unsigned long long sc = pack2(scale_log2, scale_log2), mr = minus_ref();
+#pragma unroll 1
+        for (int c = 0; c < valid; c += 32) {
+            tmem_ld32(t_s + (uint32_t)c, r);
+            tmem_ld_wait();
+            mask(r, valid - c);
+            exp_chunk<0>(r, t_p + (uint32_t)(c >> 1), sc, mr, sum, sum_b);
+        }
+        tmem_st_wait();
+        hand_over(first_half, lane);
+        return top;
+    }
+    static __device__ __forceinline__ void mask(uint32_t (&r)[32], int valid) {
+#pragma unroll
+        for (int q = 0; q < 32; ++q)
+            if (q >= valid) r[q] = __float_as_uint(-INFINITY);
+    }
+};
+
+// Item i, and the length of the one after it, whose load is under way meanwhile.
+struct Items {
+    int b, kvh, t0, streams, len, tiles;
+    int next_len;
+    uint32_t at;
+    __device__ __forceinline__ void fetch(const Params& a, uint32_t i) {
+        next_len = a.lens && i < a.items ? a.lens[i / (uint32_t)a.q_items / (uint32_t)a.Hkv] : a.Tk;
+    }
+    __device__ __forceinline__ Items(const Params& a) : at(blockIdx.x) { fetch(a, at); }
+    __device__ __forceinline__ bool take(const Params& a) {
+        if (at >= a.items) return false;
+        const uint32_t bh = at / (uint32_t)a.q_items, qt = at - bh * (uint32_t)a.q_items;
+        b = (int)(bh / (uint32_t)a.Hkv);
+        kvh = (int)bh - b * a.Hkv;
+        t0 = (int)qt * 2 * a.nt;
+        streams = t0 + a.nt < a.Tq ? 2 : 1;
+        len = min(max(next_len, 0), a.Tk);
+        tiles = (len + KEYS - 1) / KEYS;
+        at += gridDim.x;
+        fetch(a, at);
+        return true;
+    }
+};
 
 template <int DP>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
@@ -264,11 +307,12 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&bars->q_full[i]), 1); mbar_init(smem_u32(&bars->q_empty[i]), 1);
-            mbar_init(smem_u32(&bars->s_full[i]), 1); mbar_init(smem_u32(&bars->p_half[i]), SOFTMAX_WARPS / 2); mbar_init(smem_u32(&bars->p_full[i]), SOFTMAX_WARPS / 2); mbar_init(smem_u32(&bars->o_full[i]), 1);
+            mbar_init(smem_u32(&bars->q_full[i]), 1); mbar_init(smem_u32(&bars->q_empty[i]), C::MMA_WARPS);
+            mbar_init(smem_u32(&bars->s_full[i]), 1); mbar_init(smem_u32(&bars->s_free[i]), SOFTMAX_WARPS / 2);
+            for (int h = 0; h < 2; ++h) mbar_init(smem_u32(&bars->p_part[i][h]), SOFTMAX_WARPS / 2);
+            mbar_init(smem_u32(&bars->pv_done[i]), 1); mbar_init(smem_u32(&bars->o_full[i]), 1); mbar_init(smem_u32(&bars->drained[i]), 1);
         }
-        for (int i = 0; i < C::STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), 1); }
-        mbar_init(smem_u32(&bars->drained), 1);
+        for (int i = 0; i < C::STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), C::MMA_WARPS); }
         bars->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async_smem();
@@ -277,17 +321,16 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = bars->tmem_base;                   // S (and P) of tile s at 128 s, O at 256 + DP s
+    const uint32_t tmem = bars->tmem_base;
 
     if (warp < SOFTMAX_WARPS) {
         // ------------------------------------------------------------ softmax: a thread per row
         const int s = warp >> 2, row = (warp & 3) * 32 + lane;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lanes + (uint32_t)s * 128u, t_o = tmem + lanes + 256u + (uint32_t)(s * DP);
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lanes + (uint32_t)s * 128u, t_o = tmem + lanes + 256u + (uint32_t)(s * DP), t_p = tmem + lanes + C::P_COL + (uint32_t)s * C::P_STEP;
         const int tt = row / a.g, hg = row - tt * a.g;       // (once: a tile's packing is the same everywhere)
-        uint32_t n_s = 0, n_o = 0;                           // tiles and items so far
+        uint32_t n_s = 0, n_o = 0, n_pv = 0;                 // tiles, items and waited-for products so far
         bool ok = true;
-        for (int64_t i = blockIdx.x; i < a.items; i += gridDim.x) {
-            const Item it = item_of(a, i);
+        for (Items it(a); it.take(a);) {
             if (s >= it.streams) continue;
             float m_ref = -INFINITY;
             unsigned long long sum = 0, sum_b = 0;           // of even and odd pairs of keys
@@ -296,11 +339,15 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->s_full[s]), n_s & 1, abort_flag)) && ok;
                 tc_fence_after();
                 const int valid = it.len - j * KEYS;
-                const float tmax = valid >= KEYS ? softmax_full<DP>(a.scale_log2, t_s, t_o, j > 0, m_ref, sum, sum_b, &bars->p_half[s], lane)
-                                                 : softmax_part<DP>(a.scale_log2, t_s, t_o, valid, j > 0, m_ref, sum, sum_b);
+                Tile<DP> tile{a.scale_log2, t_s, t_p, t_o, j > 0, C::APART && j + 1 < it.tiles ? &bars->s_free[s] : nullptr,
+                              C::APART && j > 0 ? &bars->pv_done[s] : nullptr, n_pv & 1, abort_flag, lane, m_ref, sum, sum_b};
+                if (C::APART && j > 0) ++n_pv;
+                const float tmax = valid >= KEYS ? tile.full(&bars->p_part[s][0]) : tile.part(valid, &bars->p_part[s][0]);
+                m_ref = tile.m_ref; sum = tile.sum; sum_b = tile.sum_b;
+                ok = ok && tile.ok;
                 bad = bad || !(tmax < INFINITY);             // a NaN or an infinity among the scores
-                if (valid < KEYS) hand_over(&bars->p_half[s], lane);
-                hand_over(&bars->p_full[s], lane);
+                tmem_st_wait();
+                hand_over(&bars->p_part[s][1], lane);
             }
             if (it.tiles) {
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->o_full[s]), n_o & 1, abort_flag)) && ok;
@@ -340,8 +387,7 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
             uint32_t st = 0, ph = 0;
             int issued = 0, q_issued = 0;
             bool ok = true;
-            for (int64_t i = blockIdx.x; i < a.items && ok; i += gridDim.x) {
-                const Item it = item_of(a, i);
+            for (Items it(a); ok && it.take(a);) {
                 if (!it.tiles) continue;
                 const int buf = q_issued & 1;
                 ok = mbar_wait(smem_u32(&bars->q_empty[buf]), ((q_issued >> 1) & 1) ^ 1, abort_flag);
@@ -357,10 +403,13 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                     if (!ok) break;
                     const uint32_t full = smem_u32(&bars->full[st]);
                     mbar_arrive_expect_tx(full, C::TILE_BYTES);
+                    // K0, V0, K1, V1, ...; APART: K0, K1, V0, K2, V1, ...
+                    const bool is_v = C::APART ? j > 0 && ((j & 1) == 0 || (j + 1) / 2 == it.tiles) : (j & 1) != 0;
+                    const int tile = !C::APART ? j >> 1 : (j & 1) == 0 ? max(j / 2 - 1, 0) : is_v ? it.tiles - 1 : (j + 1) / 2;
                     for (int c = 0; c < C::CHUNKS; ++c) {
                         const uint32_t dst = smem_u32(smem_st + st * C::TILE_BYTES + c * (KEYS * 128));
-                        if (j & 1) tma_load_4d(dst, &tm_v, c * CHUNK, (j >> 1) * KEYS, it.kvh * a.vh, it.b * a.vb, full);
-                        else tma_load_4d(dst, &tm_k, c * CHUNK, (j >> 1) * KEYS, it.kvh * a.kh, it.b * a.kb, full);
+                        if (is_v) tma_load_4d(dst, &tm_v, c * CHUNK, tile * KEYS, it.kvh * a.vh, it.b * a.vb, full);
+                        else tma_load_4d(dst, &tm_k, c * CHUNK, tile * KEYS, it.kvh * a.kh, it.b * a.kb, full);
                     }
                     ++issued;
                     if (++st == C::STAGES) { st = 0; ph ^= 1; }
@@ -376,14 +425,17 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                 cc::land_loads(bars->full, C::STAGES, issued);
             }
         }
-    } else {
-        // ------------------------------------------------------------ MMA issue: the whole warp, instructions predicated on one lane
+    } else if (warp < MMA_WARP + C::MMA_WARPS) {
+        // ------------------------------------------------------------ MMA issue: the whole warp, instructions predicated on one lane.  Where P lies
+        // over the scores one warp issues for both tiles, in turn: each tile's products come between the other's, which keeps the tiles half a
+        // period apart (with a warp each they fall into step and wait for the same things: 9472 x 8192 of 128 477 -> 595 us).  Where P is apart a
+        // warp each (64: 465 -> 410).
         const uint32_t on = elect_one();
         const uint32_t n_pv = (uint32_t)((a.D + 15) & ~15);
         const uint32_t idesc_qk = make_idesc_bf16(128, KEYS), idesc_pv = make_idesc_bf16(128, n_pv) | (1u << 16);      // (bit 16: B is MN-major)
         const uint32_t hi = desc_hi(1024, 2);
         const int ksteps = (int)(n_pv >> 4);                 // of Q K^T
-        uint32_t st = 0, ph = 0, n_p[2] = {0, 0}, n_q = 0;
+        uint32_t st = 0, ph = 0, n_q = 0;
         auto wait_on = [&](uint64_t* bar, uint32_t parity) {
             const uint32_t p = smem_u32(bar);
             if (!mbar_try_wait(p, parity)) (void)mbar_wait(p, parity, abort_flag);
@@ -404,66 +456,121 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
         };
         auto issue_pv = [&](int s, uint32_t stage, int from, int steps, bool first) {
             const uint32_t v_lo = desc_lo(smem_u32(smem_st + stage * C::TILE_BYTES)) | (((KEYS * 128u) >> 4) << 16);
-            const uint32_t d = tmem + 256u + (uint32_t)(s * DP), p = tmem + (uint32_t)s * 128u;
+            const uint32_t d = tmem + 256u + (uint32_t)(s * DP), p = tmem + C::P_COL + (uint32_t)s * C::P_STEP;
 #pragma unroll
-            for (int i = 0; i < KEYS / 32; ++i) {
+            for (int i = 0; i < HALF / 16; ++i) {
                 const int k = from + i;
                 if (k >= steps) break;
                 umma_bf16_ts_on(d, p + (uint32_t)k * 8u, v_lo + (uint32_t)k * (2048u >> 4), hi, idesc_pv, first && k == 0 ? 0u : 1u, on);
             }
             __syncwarp();
         };
-        for (int64_t i = blockIdx.x; i < a.items; i += gridDim.x) {
-            const Item it = item_of(a, i);
-            if (!it.tiles) continue;
-            if (*abort_flag) break;
-            wait_on(&bars->q_full[n_q & 1], (n_q >> 1) & 1);
-            wait_on(&bars->full[st], ph);
-            for (int s = 0; s < it.streams; ++s) issue_qk(s, st);
-            commit(&bars->empty[st]);
-            if (it.tiles == 1) commit(&bars->q_empty[n_q & 1]);
-            step();
-            for (int j = 0; j < it.tiles; ++j) {
-                const uint32_t v_st = st;
-                const int valid = min(KEYS, it.len - j * KEYS), steps = (valid + 15) >> 4;
-                const bool last = j + 1 == it.tiles;
-                wait_on(&bars->full[st], ph);
-                step();
-                if (valid & 15) {                            // rows of V that count for nothing but are read
-                    for (int c = lane; c < (steps * 16 - valid) * 8; c += 32)
+        // rows of V that count for nothing but are read by the last product
+        auto clear_rows = [&](uint32_t stage, int valid, int steps) {
+            if ((valid & 15) == 0) return;
+            for (int c = lane; c < (steps * 16 - valid) * 8; c += 32)
 #pragma unroll
-                        for (int x = 0; x < C::CHUNKS; ++x)
-                            *(uint4*)(smem_st + v_st * C::TILE_BYTES + x * (KEYS * 128) + valid * 128 + c * 16) = make_uint4(0, 0, 0, 0);
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                }
-                for (int s = 0; s < it.streams; ++s) {
-                    wait_on(&bars->p_half[s], n_p[s] & 1);
-                    issue_pv(s, v_st, 0, steps, j == 0);
-                    wait_on(&bars->p_full[s], n_p[s] & 1);
-                    issue_pv(s, v_st, KEYS / 32, steps, false);
-                    ++n_p[s];
-                    if (s + 1 == it.streams) commit(&bars->empty[v_st]);
-                    if (last) {
-                        commit(&bars->o_full[s]);
-                    } else {
-                        if (s == 0) wait_on(&bars->full[st], ph);
-                        issue_qk(s, st);
-                        if (s + 1 == it.streams) {
-                            commit(&bars->empty[st]);
-                            if (j + 2 == it.tiles) commit(&bars->q_empty[n_q & 1]);
-                        }
+                for (int x = 0; x < C::CHUNKS; ++x)
+                    *(uint4*)(smem_st + stage * C::TILE_BYTES + x * (KEYS * 128) + valid * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+            fence_proxy_async_smem();
+            __syncwarp();
+        };
+        if constexpr (C::APART) {
+            const int s = warp - MMA_WARP;
+            uint32_t n_p = 0, n_f = 0;
+            for (Items it(a); it.take(a);) {
+                if (!it.tiles) continue;
+                if (*abort_flag) break;
+                wait_on(&bars->q_full[n_q & 1], (n_q >> 1) & 1);
+                if (s >= it.streams) {                       // nothing to do but to hand the stages back
+                    for (int j = 0; j < 2 * it.tiles; ++j) {
+                        wait_on(&bars->full[st], ph);
+                        if (lane == 0) mbar_arrive(smem_u32(&bars->empty[st]));
+                        step();
                     }
+                    if (lane == 0) mbar_arrive(smem_u32(&bars->q_empty[n_q & 1]));
+                    __syncwarp();
+                    ++n_q;
+                    continue;
+                }
+                auto scores = [&](bool last) {               // of the next K stage
+                    wait_on(&bars->full[st], ph);
+                    issue_qk(s, st);
+                    commit(&bars->empty[st]);
+                    if (last) commit(&bars->q_empty[n_q & 1]);
+                    step();
+                };
+                scores(it.tiles == 1);
+                for (int j = 0; j < it.tiles; ++j) {
+                    const int valid = min(KEYS, it.len - j * KEYS), steps = (valid + 15) >> 4;
+                    const bool last = j + 1 == it.tiles;
+                    if (!last) {
+                        wait_on(&bars->s_free[s], n_f & 1);
+                        ++n_f;
+                        scores(j + 2 == it.tiles);
+                    }
+                    wait_on(&bars->full[st], ph);
+                    clear_rows(st, valid, steps);            // (both warps write the same zeros)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        wait_on(&bars->p_part[s][h], n_p & 1);
+                        issue_pv(s, st, h * (HALF / 16), steps, j == 0);
+                    }
+                    ++n_p;
+                    commit(&bars->empty[st]);
+                    commit(last ? &bars->o_full[s] : &bars->pv_done[s]);
+                    step();
                     __syncwarp();
                 }
-                if (!last) step();
+                ++n_q;
             }
-            ++n_q;
+        } else {
+            uint32_t n_p[2] = {0, 0};
+            for (Items it(a); it.take(a);) {
+                if (!it.tiles) continue;
+                if (*abort_flag) break;
+                wait_on(&bars->q_full[n_q & 1], (n_q >> 1) & 1);
+                wait_on(&bars->full[st], ph);
+                for (int s = 0; s < it.streams; ++s) issue_qk(s, st);
+                commit(&bars->empty[st]);
+                if (it.tiles == 1) commit(&bars->q_empty[n_q & 1]);
+                step();
+                for (int j = 0; j < it.tiles; ++j) {
+                    const uint32_t v_st = st;
+                    const int valid = min(KEYS, it.len - j * KEYS), steps = (valid + 15) >> 4;
+                    const bool last = j + 1 == it.tiles;
+                    wait_on(&bars->full[st], ph);
+                    step();
+                    clear_rows(v_st, valid, steps);
+                    for (int s = 0; s < it.streams; ++s) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            wait_on(&bars->p_part[s][h], n_p[s] & 1);
+                            issue_pv(s, v_st, h * (HALF / 16), steps, j == 0);
+                        }
+                        ++n_p[s];
+                        if (s + 1 == it.streams) commit(&bars->empty[v_st]);
+                        if (last) {
+                            commit(&bars->o_full[s]);
+                        } else {
+                            if (s == 0) wait_on(&bars->full[st], ph);
+                            issue_qk(s, st);
+                            if (s + 1 == it.streams) {
+                                commit(&bars->empty[st]);
+                                if (j + 2 == it.tiles) commit(&bars->q_empty[n_q & 1]);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                    if (!last) step();
+                }
+                ++n_q;
+            }
         }
         if (*abort_flag) {                                   // nobody else waits for the products under way
-            commit(&bars->drained);
+            commit(&bars->drained[warp - MMA_WARP]);
             __syncwarp();
-            (void)cc::wait_cluster(smem_u32(&bars->drained), 0, abort_flag);
+            (void)cc::wait_cluster(smem_u32(&bars->drained[warp - MMA_WARP]), 0, abort_flag);
             __syncwarp();
         }
     }
@@ -478,7 +585,7 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
 template <int DP> cudaError_t launch(const Params& p, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, int sms, cudaStream_t s) {
     const cudaError_t e = cc::set_smem_limit<xattn_tc_kernel<DP>>(Cfg<DP>::SMEM);
     if (e != cudaSuccess) return e;
-    xattn_tc_kernel<DP><<<(unsigned)std::min<int64_t>(p.items, sms), NUM_THREADS, Cfg<DP>::SMEM, s>>>(p, tq, tk, tv);
+    xattn_tc_kernel<DP><<<std::min(p.items, (uint32_t)sms), NUM_THREADS, Cfg<DP>::SMEM, s>>>(p, tq, tk, tv);
     return cudaGetLastError();
 }
 
@@ -498,7 +605,7 @@ cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s) {
     p.o = a.o; p.lens = a.kv_lens;
     p.Tq = a.Tq; p.Tk = a.Tk; p.Hkv = a.Hkv; p.g = a.H / a.Hkv; p.D = a.D; p.nt = ROWS / p.g;
     p.q_items = (a.Tq + 2 * p.nt - 1) / (2 * p.nt);
-    p.items = (int64_t)p.q_items * a.Hkv * a.B;
+    p.items = (uint32_t)((int64_t)p.q_items * a.Hkv * a.B);          // (rows are at most 2^30)
     p.o_batch = a.so.batch; p.o_token = a.so.token; p.o_head = a.so.head;
     p.scale_log2 = a.scale * 1.4426950408889634f;
     const uint64_t dims[5] = {(uint64_t)a.D, (uint64_t)p.g, (uint64_t)a.Tq, (uint64_t)a.Hkv, (uint64_t)a.B};
