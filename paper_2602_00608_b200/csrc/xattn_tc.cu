@@ -28,12 +28,13 @@ using namespace tc;
 constexpr int ROWS = 128, KEYS = 128, CHUNK = 64;            // of a tile; channels of a 128-byte row
 constexpr int HALF = KEYS / 2;                               // keys of P that go to the tensor core at a time
 constexpr int SOFTMAX_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, NUM_THREADS = 352;     // MMA_WARP + s issues for tile s
+constexpr int MAX_LENS = 128;                                // lengths that are kept in shared memory
 constexpr float RESCALE_THRESHOLD = 8.0f;                    // log2 units: accumulators may grow by 2^8
 
 template <int DP> struct Cfg {
     static constexpr int CHUNKS = DP / CHUNK;
     static constexpr int TILE_BYTES = ROWS * DP * 2;         // of Q (a tile), K or V
-    static constexpr int STAGES = DP == 128 ? 3 : 6, Q_BUFS = 2;
+    static constexpr int STAGES = DP == 128 ? 3 : 6, Q_BUFS = DP == 128 ? 1 : 2;
     // Tensor memory has room for a P of its own beside the scores where O takes 64 columns: the next scores then do not wait for the
     // products of P.  Columns of tile s: S at 128 s, O at 256 + DP s, P at P_COL + P_STEP s.
     static constexpr bool APART = DP == 64;
@@ -42,22 +43,22 @@ template <int DP> struct Cfg {
     // short the issue slots are what is short.)
     static constexpr int POLY = APART ? 0 : 8;
     static constexpr int MMA_WARPS = APART ? 2 : 1;
-    static constexpr int SMEM = (Q_BUFS * 2 + STAGES) * TILE_BYTES + 512 + 1024;
+    static constexpr int SMEM = (Q_BUFS * 2 + 2 + STAGES) * TILE_BYTES + MAX_LENS * 4 + 256 + 1024;     // Q, O on its way out, K and V
 };
 struct Bars {
     uint64_t q_full[2], q_empty[2], full[6], empty[6], s_full[2], s_free[2], p_part[2][2], pv_done[2], o_full[2], drained[2];
     uint32_t tmem_base, abort_flag;
 };
-static_assert(sizeof(Bars) <= 512 && Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448, "shared memory of one CTA");
+static_assert(sizeof(Bars) <= 256 && Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448, "shared memory of one CTA");
 
 struct Params {
     void* o;
     const int32_t* lens;
-    int Tq, Tk, Hkv, g, D, nt;       // nt: tokens of a tile
+    int Tq, Tk, B, Hkv, g, D, nt;    // nt: tokens of a tile
     int q_items;                     // items of a (batch item, key head)
+    int dq, dh, db;                  // from one item of a CTA to its next: the grid as (items, heads, batch items)
     int kb, vb, kh, vh;              // 0: the batch (head) coordinate of k or v stays 0
     uint32_t items;
-    int64_t o_batch, o_token, o_head;
     float scale_log2;
 };
 
@@ -246,7 +247,7 @@ template <int DP> struct Tile {
         for (int c = 0; c < valid; c += 32) {
             tmem_ld32(t_s + (uint32_t)c, r);
             tmem_ld_wait();
-            mask(r, valid - c);
+            if (valid - c < 32) mask(r, valid - c);
             top = max_of(r, top);
         }
         wait_pv();
@@ -256,7 +257,7 @@ template <int DP> struct Tile {
         for (int c = 0; c < valid; c += 32) {
             tmem_ld32(t_s + (uint32_t)c, r);
             tmem_ld_wait();
-            mask(r, valid - c);
+            if (valid - c < 32) mask(r, valid - c);
             exp_chunk<0>(r, t_p + (uint32_t)(c >> 1), sc, mr, sum, sum_b);
         }
         tmem_st_wait();
@@ -270,26 +271,30 @@ template <int DP> struct Tile {
     }
 };
 
-// Item i, and the length of the one after it, whose load is under way meanwhile.
+// A CTA's items, one grid apart; no divisions on the way.
 struct Items {
-    int b, kvh, t0, streams, len, tiles;
-    int next_len;
+    int b, kvh, qt, t0, streams, len, tiles;
     uint32_t at;
-    __device__ __forceinline__ void fetch(const Params& a, uint32_t i) {
-        next_len = a.lens && i < a.items ? a.lens[i / (uint32_t)a.q_items / (uint32_t)a.Hkv] : a.Tk;
-    }
-    __device__ __forceinline__ Items(const Params& a) : at(blockIdx.x) { fetch(a, at); }
-    __device__ __forceinline__ bool take(const Params& a) {
-        if (at >= a.items) return false;
-        const uint32_t bh = at / (uint32_t)a.q_items, qt = at - bh * (uint32_t)a.q_items;
+    bool first = true;
+    __device__ __forceinline__ Items(const Params& a) : at(blockIdx.x) {
+        const uint32_t bh = at / (uint32_t)a.q_items;
+        qt = (int)(at - bh * (uint32_t)a.q_items);
         b = (int)(bh / (uint32_t)a.Hkv);
-        kvh = (int)bh - b * a.Hkv;
-        t0 = (int)qt * 2 * a.nt;
+        kvh = (int)(bh - (uint32_t)b * (uint32_t)a.Hkv);
+    }
+    __device__ __forceinline__ bool take(const Params& a, const int* lens) {
+        if (!first) {
+            at += gridDim.x;
+            qt += a.dq; kvh += a.dh; b += a.db;
+            if (qt >= a.q_items) { qt -= a.q_items; ++kvh; }
+            if (kvh >= a.Hkv) { kvh -= a.Hkv; ++b; }
+        }
+        first = false;
+        if (at >= a.items) return false;
+        t0 = qt * 2 * a.nt;
         streams = t0 + a.nt < a.Tq ? 2 : 1;
-        len = min(max(next_len, 0), a.Tk);
+        len = !a.lens ? a.Tk : min(max(b < MAX_LENS ? lens[b] : a.lens[b], 0), a.Tk);
         tiles = (len + KEYS - 1) / KEYS;
-        at += gridDim.x;
-        fetch(a, at);
         return true;
     }
 };
@@ -297,12 +302,14 @@ struct Items {
 template <int DP>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                const __grid_constant__ CUtensorMap tm_v) {
+                const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o) {
     using C = Cfg<DP>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem_q = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint8_t* smem_st = smem_q + C::Q_BUFS * 2 * C::TILE_BYTES;
-    Bars* bars = (Bars*)(smem_st + C::STAGES * C::TILE_BYTES);
+    uint8_t* smem_o = smem_q + C::Q_BUFS * 2 * C::TILE_BYTES;
+    uint8_t* smem_st = smem_o + 2 * C::TILE_BYTES;
+    int* lens = (int*)(smem_st + C::STAGES * C::TILE_BYTES);
+    Bars* bars = (Bars*)(lens + MAX_LENS);
     volatile uint32_t* abort_flag = &bars->abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
@@ -317,6 +324,7 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async_smem();
     }
+    if (a.lens && tid < min(a.B, MAX_LENS)) lens[tid] = a.lens[tid];
     if (warp == MMA_WARP) tmem_alloc(smem_u32(&bars->tmem_base), 512);
     tc_fence_before();
     __syncthreads();
@@ -327,10 +335,11 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
         // ------------------------------------------------------------ softmax: a thread per row
         const int s = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lanes + (uint32_t)s * 128u, t_o = tmem + lanes + 256u + (uint32_t)(s * DP), t_p = tmem + lanes + C::P_COL + (uint32_t)s * C::P_STEP;
-        const int tt = row / a.g, hg = row - tt * a.g;       // (once: a tile's packing is the same everywhere)
+        uint8_t* out = smem_o + s * C::TILE_BYTES + row * 128;
+        const bool out_thread = (tid & (ROWS - 1)) == 0;
         uint32_t n_s = 0, n_o = 0, n_pv = 0;                 // tiles, items and waited-for products so far
         bool ok = true;
-        for (Items it(a); it.take(a);) {
+        for (Items it(a); it.take(a, lens);) {
             if (s >= it.streams) continue;
             float m_ref = -INFINITY;
             unsigned long long sum = 0, sum_b = 0;           // of even and odd pairs of keys
@@ -355,42 +364,50 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                 ++n_o;
             }
             const float inv = it.tiles == 0 ? 0.f : ok && !bad ? 1.f / sum2(add2(sum, sum_b)) : __int_as_float(0x7fffffff);
-            const int t = it.t0 + s * a.nt + tt;
-            const bool inside = tt < a.nt && t < a.Tq;
-            __nv_bfloat16* o = (__nv_bfloat16*)a.o + it.b * a.o_batch + t * a.o_token + (it.kvh * a.g + hg) * a.o_head;
+            // the rows through shared memory (swizzled like the operands), out by a bulk tensor store that the next item's softmax does not wait
+            // for: rows written straight from the threads, a line each, held the load/store unit for 2000 cycles an item
+            if (out_thread) bulk_wait_group_read<0>();       // the last item's rows have left
+            named_barrier_sync(1 + s, ROWS);
 #pragma unroll
-            for (int c = 0; c < DP; c += 32) {
-                if (c >= a.D) break;
-                uint32_t v[32];
-                if (it.tiles) {
-                    tmem_ld32(t_o + (uint32_t)c, v);
-                    tmem_ld_wait();
-                } else {
+            for (int c = 0; c < DP; c += 32)
+                if (c < a.D) {
+                    uint32_t v[32];
+                    if (it.tiles) {
+                        tmem_ld32(t_o + (uint32_t)c, v);
+                        tmem_ld_wait();
+                    } else {
 #pragma unroll
-                    for (int q = 0; q < 32; ++q) v[q] = 0u;
-                }
-                if (inside)
+                        for (int q = 0; q < 32; ++q) v[q] = 0u;
+                    }
 #pragma unroll
                     for (int q = 0; q < 32; q += 8) {
-                        if (c + q >= a.D) break;
                         float f[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(v[q + e]) * inv;
-                        *(uint4*)(o + c + q) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+                        *(uint4*)(out + (c / 64) * (ROWS * 128) + (((uint32_t)((c % 64 + q) / 8) ^ (uint32_t)(row & 7)) << 4)) =
+                            make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
                     }
+                }
+            fence_proxy_async_smem();
+            named_barrier_sync(1 + s, ROWS);
+            if (out_thread) {
+                for (int c = 0; c < C::CHUNKS; ++c)
+                    tma_store_5d(&tm_o, smem_u32(smem_o + s * C::TILE_BYTES + c * (ROWS * 128)), c * CHUNK, 0, it.t0 + s * a.nt, it.kvh, it.b);
+                bulk_commit_group();
             }
             tc_fence_before();                               // (the next product into O waits for this warp's next P)
         }
+        if (out_thread) bulk_wait_group_read<0>();           // before the CTA's memory goes
     } else if (warp == LOAD_WARP) {
         // ------------------------------------------------------------ loads: Q, then K and V of each tile in turn
         if (lane == 0) {
             uint32_t st = 0, ph = 0;
             int issued = 0, q_issued = 0;
             bool ok = true;
-            for (Items it(a); ok && it.take(a);) {
+            for (Items it(a); ok && it.take(a, lens);) {
                 if (!it.tiles) continue;
-                const int buf = q_issued & 1;
-                ok = mbar_wait(smem_u32(&bars->q_empty[buf]), ((q_issued >> 1) & 1) ^ 1, abort_flag);
+                const int buf = q_issued % C::Q_BUFS;
+                ok = mbar_wait(smem_u32(&bars->q_empty[buf]), ((q_issued / C::Q_BUFS) & 1) ^ 1, abort_flag);
                 if (!ok) break;
                 const uint32_t qf = smem_u32(&bars->q_full[buf]);
                 mbar_arrive_expect_tx(qf, (uint32_t)(it.streams * C::CHUNKS * a.g * a.nt * 128));
@@ -421,7 +438,7 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                 if (ok && ++st == C::STAGES) { st = 0; ph ^= 1; }
             }
             if (!ok) {
-                cc::land_loads(bars->q_full, 2, q_issued);
+                cc::land_loads(bars->q_full, C::Q_BUFS, q_issued);
                 cc::land_loads(bars->full, C::STAGES, issued);
             }
         }
@@ -444,7 +461,7 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
         auto commit = [&](uint64_t* bar) { umma_commit_on(smem_u32(bar), on); };
         auto step = [&]() { if (++st == C::STAGES) { st = 0; ph ^= 1; } };
         auto issue_qk = [&](int s, uint32_t stage) {
-            const uint32_t q_lo = desc_lo(smem_u32(smem_q + ((n_q & 1) * 2 + s) * C::TILE_BYTES)), k_lo = desc_lo(smem_u32(smem_st + stage * C::TILE_BYTES));
+            const uint32_t q_lo = desc_lo(smem_u32(smem_q + ((n_q % C::Q_BUFS) * 2 + s) * C::TILE_BYTES)), k_lo = desc_lo(smem_u32(smem_st + stage * C::TILE_BYTES));
 #pragma unroll
             for (int k = 0; k < DP / 16; ++k) {
                 if (k >= ksteps) break;
@@ -478,17 +495,17 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
         if constexpr (C::APART) {
             const int s = warp - MMA_WARP;
             uint32_t n_p = 0, n_f = 0;
-            for (Items it(a); it.take(a);) {
+            for (Items it(a); it.take(a, lens);) {
                 if (!it.tiles) continue;
                 if (*abort_flag) break;
-                wait_on(&bars->q_full[n_q & 1], (n_q >> 1) & 1);
+                wait_on(&bars->q_full[n_q % C::Q_BUFS], (n_q / C::Q_BUFS) & 1);
                 if (s >= it.streams) {                       // nothing to do but to hand the stages back
                     for (int j = 0; j < 2 * it.tiles; ++j) {
                         wait_on(&bars->full[st], ph);
                         if (lane == 0) mbar_arrive(smem_u32(&bars->empty[st]));
                         step();
                     }
-                    if (lane == 0) mbar_arrive(smem_u32(&bars->q_empty[n_q & 1]));
+                    if (lane == 0) mbar_arrive(smem_u32(&bars->q_empty[n_q % C::Q_BUFS]));
                     __syncwarp();
                     ++n_q;
                     continue;
@@ -497,7 +514,7 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                     wait_on(&bars->full[st], ph);
                     issue_qk(s, st);
                     commit(&bars->empty[st]);
-                    if (last) commit(&bars->q_empty[n_q & 1]);
+                    if (last) commit(&bars->q_empty[n_q % C::Q_BUFS]);
                     step();
                 };
                 scores(it.tiles == 1);
@@ -526,14 +543,14 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
             }
         } else {
             uint32_t n_p[2] = {0, 0};
-            for (Items it(a); it.take(a);) {
+            for (Items it(a); it.take(a, lens);) {
                 if (!it.tiles) continue;
                 if (*abort_flag) break;
-                wait_on(&bars->q_full[n_q & 1], (n_q >> 1) & 1);
+                wait_on(&bars->q_full[n_q % C::Q_BUFS], (n_q / C::Q_BUFS) & 1);
                 wait_on(&bars->full[st], ph);
                 for (int s = 0; s < it.streams; ++s) issue_qk(s, st);
                 commit(&bars->empty[st]);
-                if (it.tiles == 1) commit(&bars->q_empty[n_q & 1]);
+                if (it.tiles == 1) commit(&bars->q_empty[n_q % C::Q_BUFS]);
                 step();
                 for (int j = 0; j < it.tiles; ++j) {
                     const uint32_t v_st = st;
@@ -557,7 +574,7 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                             issue_qk(s, st);
                             if (s + 1 == it.streams) {
                                 commit(&bars->empty[st]);
-                                if (j + 2 == it.tiles) commit(&bars->q_empty[n_q & 1]);
+                                if (j + 2 == it.tiles) commit(&bars->q_empty[n_q % C::Q_BUFS]);
                             }
                         }
                         __syncwarp();
@@ -582,10 +599,24 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
     }
 }
 
-template <int DP> cudaError_t launch(const Params& p, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, int sms, cudaStream_t s) {
+// q or o as [D, heads of a key head, tokens, key heads, batch], in boxes of nt tokens
+bool encode_rows(CUtensorMap* tm, const XAttnArgs& a, const void* p, const Strides& s, int nt) {
+    const int g = a.H / a.Hkv;
+    const uint64_t dims[5] = {(uint64_t)a.D, (uint64_t)g, (uint64_t)a.Tq, (uint64_t)a.Hkv, (uint64_t)a.B};
+    uint64_t st[4];
+    const uint32_t box[5] = {CHUNK, (uint32_t)g, (uint32_t)nt, 1, 1};
+    return stride_ok(s.head, g, &st[0]) && stride_ok(s.token, a.Tq, &st[1]) && stride_ok(s.head * g, a.Hkv, &st[2]) && stride_ok(s.batch, a.B, &st[3]) &&
+           encode_map(tm, p, 5, dims, st, box);
+}
+
+template <int DP> cudaError_t launch(Params& p, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& to, int sms, cudaStream_t s) {
     const cudaError_t e = cc::set_smem_limit<xattn_tc_kernel<DP>>(Cfg<DP>::SMEM);
     if (e != cudaSuccess) return e;
-    xattn_tc_kernel<DP><<<std::min(p.items, (uint32_t)sms), NUM_THREADS, Cfg<DP>::SMEM, s>>>(p, tq, tk, tv);
+    const uint32_t grid = std::min(p.items, (uint32_t)sms), heads = grid / (uint32_t)p.q_items;
+    p.dq = (int)(grid % (uint32_t)p.q_items);
+    p.dh = (int)(heads % (uint32_t)p.Hkv);
+    p.db = (int)(heads / (uint32_t)p.Hkv);
+    xattn_tc_kernel<DP><<<grid, NUM_THREADS, Cfg<DP>::SMEM, s>>>(p, tq, tk, tv, to);
     return cudaGetLastError();
 }
 
@@ -594,32 +625,29 @@ template <int DP> cudaError_t launch(const Params& p, const CUtensorMap& tq, con
 bool xattn_tc_supported(const XAttnArgs& a) {
     const int g = a.H / a.Hkv;
     uint64_t unused;
-    return kv_maps_supported(a) && g <= ROWS && (((uintptr_t)a.q | (uintptr_t)a.o) & 15) == 0 && ((a.so.batch | a.so.token | a.so.head) & 7) == 0 &&
-           stride_ok(a.sq.head, a.H, &unused) && stride_ok(a.sq.token, a.Tq, &unused) && stride_ok(a.sq.batch, a.B, &unused) &&
-           a.sq.head < (1ll << 38) / std::max(g, 1);
+    const auto rows_ok = [&](const void* p, const Strides& s) {
+        return ((uintptr_t)p & 15) == 0 && stride_ok(s.head, a.H, &unused) && stride_ok(s.token, a.Tq, &unused) && stride_ok(s.batch, a.B, &unused) &&
+               s.head < (1ll << 38) / std::max(g, 1);
+    };
+    return kv_maps_supported(a) && g <= ROWS && rows_ok(a.q, a.sq) && rows_ok(a.o, a.so);
 }
 
 cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s) {
-    CUtensorMap tq, tk, tv;
+    CUtensorMap tq, tk, tv, to;
     Params p;
     p.o = a.o; p.lens = a.kv_lens;
-    p.Tq = a.Tq; p.Tk = a.Tk; p.Hkv = a.Hkv; p.g = a.H / a.Hkv; p.D = a.D; p.nt = ROWS / p.g;
+    p.Tq = a.Tq; p.Tk = a.Tk; p.B = a.B; p.Hkv = a.Hkv; p.g = a.H / a.Hkv; p.D = a.D; p.nt = ROWS / p.g;
     p.q_items = (a.Tq + 2 * p.nt - 1) / (2 * p.nt);
     p.items = (uint32_t)((int64_t)p.q_items * a.Hkv * a.B);          // (rows are at most 2^30)
-    p.o_batch = a.so.batch; p.o_token = a.so.token; p.o_head = a.so.head;
     p.scale_log2 = a.scale * 1.4426950408889634f;
-    const uint64_t dims[5] = {(uint64_t)a.D, (uint64_t)p.g, (uint64_t)a.Tq, (uint64_t)a.Hkv, (uint64_t)a.B};
-    uint64_t st[4];
-    const uint32_t box[5] = {CHUNK, (uint32_t)p.g, (uint32_t)p.nt, 1, 1};
-    if (!stride_ok(a.sq.head, p.g, &st[0]) || !stride_ok(a.sq.token, a.Tq, &st[1]) || !stride_ok(a.sq.head * p.g, a.Hkv, &st[2]) ||
-        !stride_ok(a.sq.batch, a.B, &st[3]) || !encode_map(&tq, a.q, 5, dims, st, box) || !encode_kv(&tk, a, a.k, a.sk, KEYS, &p.kh, &p.kb) ||
+    if (!encode_rows(&tq, a, a.q, a.sq, p.nt) || !encode_rows(&to, a, a.o, a.so, p.nt) || !encode_kv(&tk, a, a.k, a.sk, KEYS, &p.kh, &p.kb) ||
         !encode_kv(&tv, a, a.v, a.sv, KEYS, &p.vh, &p.vb))
         return cudaErrorInvalidValue;
     int dev = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
-    return a.D <= 64 ? launch<64>(p, tq, tk, tv, sms, s) : launch<128>(p, tq, tk, tv, sms, s);
+    return a.D <= 64 ? launch<64>(p, tq, tk, tv, to, sms, s) : launch<128>(p, tq, tk, tv, to, sms, s);
 }
 
 }  // namespace vd
