@@ -109,13 +109,17 @@ __device__ __forceinline__ void umma_bf16_ts_on(uint32_t d_tmem, uint32_t a_tmem
         ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(on) : "memory");
 }
 
-// 32 scores into 32 numbers of P: 2^(score * scale - reference), their sums, bf16; every POLY-th pair on the FMA pipes
-template <int POLY>
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+// N = 32 or 16 scores into as many numbers of P: 2^(score * scale - reference), their sums, bf16; every POLY-th pair on the FMA pipes
+template <int POLY, int N = 32>
 __device__ __forceinline__ void exp_chunk(const uint32_t (&r)[32], uint32_t t_p, unsigned long long sc, unsigned long long mr,
                                           unsigned long long& sum, unsigned long long& sum_b) {
     uint32_t pk[16];
 #pragma unroll
-    for (int q = 0; q < 32; q += 2) {
+    for (int q = 0; q < N; q += 2) {
         float e0, e1;
         unpack2(fmaf2(pack2(__uint_as_float(r[q]), __uint_as_float(r[q + 1])), sc, mr), e0, e1);
         if (POLY && (q / 2) % (POLY ? POLY : 1) == POLY - 1) {
@@ -128,7 +132,8 @@ __device__ __forceinline__ void exp_chunk(const uint32_t (&r)[32], uint32_t t_p,
         else sum = add2(sum, pack2(e0, e1));
         pk[q >> 1] = pack_bf16(e0, e1);
     }
-    tmem_st16(t_p, pk);
+    if (N == 32) tmem_st16(t_p, pk);
+    else tmem_st8(t_p, pk);
 }
 __device__ __forceinline__ float max_of(const uint32_t (&r)[32], float m) {
     float a = max3(__uint_as_float(r[0]), __uint_as_float(r[1]), m), b = max3(__uint_as_float(r[2]), __uint_as_float(r[3]), __uint_as_float(r[4]));
@@ -239,7 +244,38 @@ template <int DP> struct Tile {
         exp_chunk<POLY>(a, t_p + 48u, sc, mr, sum, sum_b);
         return t1;
     }
-    // Only the first `valid` keys count: the others leave before the maximum.  (The code of full() with masks spills in both.)
+    // The same where only the first `valid` <= 96 keys count: the others leave before the maximum, 16 keys are the least that is worked on.
+    __device__ __forceinline__ float most(int valid, uint64_t* first_half) {
+        constexpr int POLY = 4;
+        uint32_t a[32], b[32], c[32];
+        tmem_ld32(t_s, a);
+        tmem_ld32(t_s + 32u, b);
+        tmem_ld32(t_s + 64u, c);
+        tmem_ld_wait();
+        if (valid < 32) mask(a, valid);
+        float top = max_of(a, -INFINITY);
+        if (valid > 32) {
+            if (valid < 64) mask(b, valid - 32);
+            top = max_of(b, top);
+        }
+        if (valid > 64) {
+            if (valid < 96) mask(c, valid - 64);
+            top = max_of(c, top);
+        }
+        wait_pv();
+        move_reference(top * scale_log2, 0u);
+        const unsigned long long sc = pack2(scale_log2, scale_log2), mr = minus_ref();
+        if (valid > 16) exp_chunk<POLY>(a, t_p, sc, mr, sum, sum_b);
+        else exp_chunk<POLY, 16>(a, t_p, sc, mr, sum, sum_b);
+        if (valid > 48) exp_chunk<POLY>(b, t_p + 16u, sc, mr, sum, sum_b);
+        else if (valid > 32) exp_chunk<POLY, 16>(b, t_p + 16u, sc, mr, sum, sum_b);
+        tmem_st_wait();
+        hand_over(first_half, lane);
+        if (valid > 80) exp_chunk<POLY>(c, t_p + 32u, sc, mr, sum, sum_b);
+        else if (valid > 64) exp_chunk<POLY, 16>(c, t_p + 32u, sc, mr, sum, sum_b);
+        return top;
+    }
+    // The same for any number of them, 32 at a time.  (The code of full() with masks spills.)
     __device__ __forceinline__ float part(int valid, uint64_t* first_half) {
         uint32_t r[32];
         float top = -INFINITY;
@@ -351,7 +387,8 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                 Tile<DP> tile{a.scale_log2, t_s, t_p, t_o, j > 0, C::APART && j + 1 < it.tiles ? &bars->s_free[s] : nullptr,
                               C::APART && j > 0 ? &bars->pv_done[s] : nullptr, n_pv & 1, abort_flag, lane, m_ref, sum, sum_b};
                 if (C::APART && j > 0) ++n_pv;
-                const float tmax = valid >= KEYS ? tile.full(&bars->p_part[s][0]) : tile.part(valid, &bars->p_part[s][0]);
+                const float tmax = valid >= KEYS ? tile.full(&bars->p_part[s][0]) : valid <= 96 ? tile.most(valid, &bars->p_part[s][0])
+                                                                                            : tile.part(valid, &bars->p_part[s][0]);
                 m_ref = tile.m_ref; sum = tile.sum; sum_b = tile.sum_b;
                 ok = ok && tile.ok;
                 bad = bad || !(tmax < INFINITY);             // a NaN or an infinity among the scores
