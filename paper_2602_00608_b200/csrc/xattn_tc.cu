@@ -19,6 +19,7 @@
 #include "conv_cluster.cuh"
 #include "tc_common.cuh"
 #include "xattn_maps.h"
+#include "xattn_meet.cuh"
 
 namespace vd {
 namespace {
@@ -29,6 +30,8 @@ constexpr int ROWS = 128, KEYS = 128, CHUNK = 64;            // of a tile; chann
 constexpr int HALF = KEYS / 2;                               // keys of P that go to the tensor core at a time
 constexpr int SOFTMAX_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, NUM_THREADS = 352;     // MMA_WARP + s issues for tile s
 constexpr int MAX_LENS = 128;                                // lengths that are kept in shared memory
+constexpr int MAX_SPLITS = xa::MAX_SPLITS;
+constexpr double MEET_TILES = 4.0;                           // what a meeting costs, in tiles
 constexpr float RESCALE_THRESHOLD = 8.0f;                    // log2 units: accumulators may grow by 2^8
 
 template <int DP> struct Cfg {
@@ -43,22 +46,24 @@ template <int DP> struct Cfg {
     // short the issue slots are what is short.)
     static constexpr int POLY = APART ? 0 : 8;
     static constexpr int MMA_WARPS = APART ? 2 : 1;
-    static constexpr int SMEM = (Q_BUFS * 2 + 2 + STAGES) * TILE_BYTES + MAX_LENS * 4 + 256 + 1024;     // Q, O on its way out, K and V
+    static constexpr int SMEM = (Q_BUFS * 2 + 2 + STAGES) * TILE_BYTES + 2 * ROWS * 8 + MAX_LENS * 4 + 320;     // Q, O on its way out, K and V; (reference, sum) of the rows
 };
 struct Bars {
-    uint64_t q_full[2], q_empty[2], full[6], empty[6], s_full[2], s_free[2], p_part[2][2], pv_done[2], o_full[2], drained[2];
+    uint64_t q_full[2], q_empty[2], full[6], empty[6], s_full[2], s_free[2], p_part[2][2], pv_done[2], o_full[2], drained[2], shown[2], seen[2];
     uint32_t tmem_base, abort_flag;
 };
-static_assert(sizeof(Bars) <= 256 && Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448, "shared memory of one CTA");
+static_assert(sizeof(Bars) <= 320 && Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448, "shared memory of one CTA");
 
 struct Params {
-    void* o;
     const int32_t* lens;
     int Tq, Tk, B, Hkv, g, D, nt;    // nt: tokens of a tile
     int q_items;                     // items of a (batch item, key head)
     int dq, dh, db;                  // from one item of a CTA to its next: the grid as (items, heads, batch items)
     int kb, vb, kh, vh;              // 0: the batch (head) coordinate of k or v stays 0
-    uint32_t items;
+    uint32_t items, whole;           // the first `whole` items are a CTA's each, the others a cluster's, whose CTAs divide the keys
+    int splits;                      // CTAs of a cluster
+    __nv_bfloat16* o;
+    int64_t o_batch, o_token, o_head;
     float scale_log2;
 };
 
@@ -307,44 +312,138 @@ template <int DP> struct Tile {
     }
 };
 
-// A CTA's items, one grid apart; no divisions on the way.
-struct Items {
-    int b, kvh, qt, t0, streams, len, tiles;
+// A CTA's items: of the whole ones those one grid apart (no divisions on the way), then its share of the keys of its cluster's.
+template <bool SPLIT> struct Items {
+    int b, kvh, qt, t0, streams, len, tiles;     // tiles of the item, of which [j0, j0 + n) are this CTA's
+    int j0, n;
     uint32_t at;
-    bool first = true;
-    __device__ __forceinline__ Items(const Params& a) : at(blockIdx.x) {
+    bool first = true, split = false;        // (without SPLIT all items are whole)
+    __device__ __forceinline__ void place(const Params& a) {
         const uint32_t bh = at / (uint32_t)a.q_items;
         qt = (int)(at - bh * (uint32_t)a.q_items);
         b = (int)(bh / (uint32_t)a.Hkv);
         kvh = (int)(bh - (uint32_t)b * (uint32_t)a.Hkv);
     }
+    __device__ __forceinline__ Items(const Params& a) : at(blockIdx.x) { place(a); }
     __device__ __forceinline__ bool take(const Params& a, const int* lens) {
-        if (!first) {
-            at += gridDim.x;
-            qt += a.dq; kvh += a.dh; b += a.db;
-            if (qt >= a.q_items) { qt -= a.q_items; ++kvh; }
-            if (kvh >= a.Hkv) { kvh -= a.Hkv; ++b; }
+        if (!SPLIT || !split) {
+            if (!first) {
+                at += gridDim.x;
+                qt += a.dq; kvh += a.dh; b += a.db;
+                if (qt >= a.q_items) { qt -= a.q_items; ++kvh; }
+                if (kvh >= a.Hkv) { kvh -= a.Hkv; ++b; }
+            }
+            first = false;
+            if (SPLIT && at >= a.whole) {
+                split = true;
+                at = a.whole + blockIdx.x / (uint32_t)a.splits;
+                place(a);
+            }
+        } else {
+            at += gridDim.x / (uint32_t)a.splits;
+            place(a);
         }
-        first = false;
         if (at >= a.items) return false;
         t0 = qt * 2 * a.nt;
         streams = t0 + a.nt < a.Tq ? 2 : 1;
         len = !a.lens ? a.Tk : min(max(b < MAX_LENS ? lens[b] : a.lens[b], 0), a.Tk);
         tiles = (len + KEYS - 1) / KEYS;
+        j0 = 0;
+        n = tiles;
+        if (SPLIT && split) {                                // (at most 2^23 tiles, 8 shares)
+            const int rank = (int)(blockIdx.x % (uint32_t)a.splits);
+            j0 = tiles * rank / a.splits;
+            n = tiles * (rank + 1) / a.splits - j0;
+        }
         return true;
     }
 };
-
+__device__ __forceinline__ void arrive_release_cluster(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+// The CTAs of a cluster have each taken a share of an item's keys: they show one another half of the channels at a time, in fp32, and each
+// adds up (in the order of the shares) and writes its part of the tile's rows.  By the 128 threads of tile s; `rounds` counts what these
+// have shown so far.  Out of line: few items come here, and the softmax has no registers to spare.
 template <int DP>
+__device__ __noinline__ void meet(const Params& a, const Items<true>& it, Bars* bars, uint8_t* show, float2* ml, float2 mine, uint32_t t_o, int s, int row, uint32_t rounds) {
+    constexpr int COLS = DP / 2, PIECES = COLS / 4;          // of a round; 16-byte pieces of them
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+    const int rank = (int)cluster_ctarank();
+    auto tell = [&](uint64_t* bar) {
+        named_barrier_sync(1 + s, ROWS);
+        if (row < a.splits) arrive_release_cluster(map_to_cta(smem_u32(bar), (uint32_t)row));
+    };
+    auto hear = [&](uint64_t* bar, uint32_t parity) {
+        (void)cc::wait_cluster(smem_u32(bar), parity, abort_flag);
+        __syncwarp();
+    };
+    for (int round = 0; round < 2; ++round, ++rounds) {
+        if (rounds > 0) hear(&bars->seen[s], (rounds - 1) & 1);      // everybody has read what was shown last
+        if (round == 0) ml[row] = mine;
+#pragma unroll
+        for (int c = 0; c < COLS; c += 32) {
+            uint32_t v[32];
+            if (it.n) {
+                tmem_ld32(t_o + (uint32_t)(round * COLS + c), v);
+                tmem_ld_wait();
+            } else {
+#pragma unroll
+                for (int q = 0; q < 32; ++q) v[q] = 0u;
+            }
+#pragma unroll
+            for (int q = 0; q < 32; q += 4)
+                *(uint4*)(show + row * (COLS * 4) + ((((c + q) >> 2) ^ (row & (PIECES - 1))) << 4)) = make_uint4(v[q], v[q + 1], v[q + 2], v[q + 3]);
+        }
+        tell(&bars->shown[s]);
+        hear(&bars->shown[s], rounds & 1);
+        const int r0 = ROWS * rank / a.splits, r1 = ROWS * (rank + 1) / a.splits;
+        for (int i = r0 * PIECES + row; i < r1 * PIECES; i += ROWS) {
+            const int r = i / PIECES, piece = i % PIECES, tt = r / a.g, t = it.t0 + s * a.nt + tt, d = round * COLS + piece * 4;
+            if (tt >= a.nt || t >= a.Tq || d >= a.D) continue;
+            const uint32_t at = smem_u32(show + r * (COLS * 4) + ((piece ^ (r & (PIECES - 1))) << 4)), at_ml = smem_u32(ml + r);
+            float top = -INFINITY;
+            for (int k = 0; k < a.splits; ++k) top = fmaxf(top, ld_cluster2(map_to_cta(at_ml, (uint32_t)k)).x);
+            const float ref = top == -INFINITY ? 0.f : top;
+            float l = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k = 0; k < a.splits; ++k) {
+                const float2 w = ld_cluster2(map_to_cta(at_ml, (uint32_t)k));
+                const float4 v = ld_cluster4(map_to_cta(at, (uint32_t)k));
+                const float f = ex2(w.x - ref);
+                l = fmaf(f, w.y, l);
+                o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+            }
+            const float inv = 1.f / l;
+            *(uint2*)(a.o + it.b * a.o_batch + t * a.o_token + (it.kvh * a.g + r - tt * a.g) * a.o_head + d) =
+                make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        }
+        tell(&bars->seen[s]);
+    }
+}
+
+// SPLIT: some items are divided by keys among the CTAs of a cluster (a build of its own: the code costs the short items 20 % even where it is
+// not reached)
+template <int DP, bool SPLIT>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
-xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                 const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o) {
     using C = Cfg<DP>;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem_q = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    extern __shared__ __align__(1024) uint8_t smem_q[];
+    if (smem_u32(smem_q) & 1023u) return;                    // (it is: the swizzle needs it)
     uint8_t* smem_o = smem_q + C::Q_BUFS * 2 * C::TILE_BYTES;
     uint8_t* smem_st = smem_o + 2 * C::TILE_BYTES;
-    int* lens = (int*)(smem_st + C::STAGES * C::TILE_BYTES);
+    float2* ml = (float2*)(smem_st + C::STAGES * C::TILE_BYTES);         // [2][ROWS]
+    int* lens = (int*)(ml + 2 * ROWS);
     Bars* bars = (Bars*)(lens + MAX_LENS);
     volatile uint32_t* abort_flag = &bars->abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -354,6 +453,7 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
             mbar_init(smem_u32(&bars->s_full[i]), 1); mbar_init(smem_u32(&bars->s_free[i]), SOFTMAX_WARPS / 2);
             for (int h = 0; h < 2; ++h) mbar_init(smem_u32(&bars->p_part[i][h]), SOFTMAX_WARPS / 2);
             mbar_init(smem_u32(&bars->pv_done[i]), 1); mbar_init(smem_u32(&bars->o_full[i]), 1); mbar_init(smem_u32(&bars->drained[i]), 1);
+            mbar_init(smem_u32(&bars->shown[i]), (uint32_t)a.splits); mbar_init(smem_u32(&bars->seen[i]), (uint32_t)a.splits);
         }
         for (int i = 0; i < C::STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), C::MMA_WARPS); }
         bars->abort_flag = 0;
@@ -364,6 +464,7 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
     if (warp == MMA_WARP) tmem_alloc(smem_u32(&bars->tmem_base), 512);
     tc_fence_before();
     __syncthreads();
+    if (SPLIT) cluster_sync_all();                    // every CTA's barriers exist before another one arrives on them
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
 
@@ -373,18 +474,18 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lanes + (uint32_t)s * 128u, t_o = tmem + lanes + 256u + (uint32_t)(s * DP), t_p = tmem + lanes + C::P_COL + (uint32_t)s * C::P_STEP;
         uint8_t* out = smem_o + s * C::TILE_BYTES + row * 128;
         const bool out_thread = (tid & (ROWS - 1)) == 0;
-        uint32_t n_s = 0, n_o = 0, n_pv = 0;                 // tiles, items and waited-for products so far
+        uint32_t n_s = 0, n_o = 0, n_pv = 0, n_meet = 0;     // tiles, items, waited-for products and rounds of meetings so far
         bool ok = true;
-        for (Items it(a); it.take(a, lens);) {
-            if (s >= it.streams) continue;
+        for (Items<SPLIT> it(a); it.take(a, lens);) {
+            if (s >= it.streams || (SPLIT && it.split && it.tiles == 0 && blockIdx.x % (uint32_t)a.splits != 0)) continue;
             float m_ref = -INFINITY;
             unsigned long long sum = 0, sum_b = 0;           // of even and odd pairs of keys
             bool bad = false;
-            for (int j = 0; j < it.tiles; ++j, ++n_s) {
+            for (int j = 0; j < it.n; ++j, ++n_s) {
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->s_full[s]), n_s & 1, abort_flag)) && ok;
                 tc_fence_after();
-                const int valid = it.len - j * KEYS;
-                Tile<DP> tile{a.scale_log2, t_s, t_p, t_o, j > 0, C::APART && j + 1 < it.tiles ? &bars->s_free[s] : nullptr,
+                const int valid = it.len - (it.j0 + j) * KEYS;
+                Tile<DP> tile{a.scale_log2, t_s, t_p, t_o, j > 0, C::APART && j + 1 < it.n ? &bars->s_free[s] : nullptr,
                               C::APART && j > 0 ? &bars->pv_done[s] : nullptr, n_pv & 1, abort_flag, lane, m_ref, sum, sum_b};
                 if (C::APART && j > 0) ++n_pv;
                 const float tmax = valid >= KEYS ? tile.full(&bars->p_part[s][0]) : valid <= 96 ? tile.most(valid, &bars->p_part[s][0])
@@ -395,15 +496,30 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                 tmem_st_wait();
                 hand_over(&bars->p_part[s][1], lane);
             }
-            if (it.tiles) {
+            if (it.n) {
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->o_full[s]), n_o & 1, abort_flag)) && ok;
                 tc_fence_after();
                 ++n_o;
             }
-            const float inv = it.tiles == 0 ? 0.f : ok && !bad ? 1.f / sum2(add2(sum, sum_b)) : __int_as_float(0x7fffffff);
+            const float l = ok && !bad ? sum2(add2(sum, sum_b)) : __int_as_float(0x7fffffff);
+            if constexpr (SPLIT) {
+                if (it.split && it.tiles) {
+                    if (out_thread) bulk_wait_group_read<0>();
+                    named_barrier_sync(1 + s, ROWS);
+                    meet<DP>(a, it, bars, smem_o + s * C::TILE_BYTES, ml + s * ROWS, make_float2(m_ref, it.n ? l : 0.f), t_o, s, row, n_meet);
+                    n_meet += 2;
+                    tc_fence_before();
+                    continue;
+                }
+            }
+            const float inv = it.tiles ? 1.f / l : 0.f;
             // the rows through shared memory (swizzled like the operands), out by a bulk tensor store that the next item's softmax does not wait
             // for: rows written straight from the threads, a line each, held the load/store unit for 2000 cycles an item
             if (out_thread) bulk_wait_group_read<0>();       // the last item's rows have left
+            if (SPLIT && n_meet) {                           // and what was shown at the last meeting has been read
+                (void)cc::wait_cluster(smem_u32(&bars->seen[s]), (n_meet - 1) & 1, abort_flag);
+                __syncwarp();
+            }
             named_barrier_sync(1 + s, ROWS);
 #pragma unroll
             for (int c = 0; c < DP; c += 32)
@@ -441,8 +557,8 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
             uint32_t st = 0, ph = 0;
             int issued = 0, q_issued = 0;
             bool ok = true;
-            for (Items it(a); ok && it.take(a, lens);) {
-                if (!it.tiles) continue;
+            for (Items<SPLIT> it(a); ok && it.take(a, lens);) {
+                if (!it.n) continue;
                 const int buf = q_issued % C::Q_BUFS;
                 ok = mbar_wait(smem_u32(&bars->q_empty[buf]), ((q_issued / C::Q_BUFS) & 1) ^ 1, abort_flag);
                 if (!ok) break;
@@ -452,14 +568,14 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                     for (int c = 0; c < C::CHUNKS; ++c)
                         tma_load_5d(smem_u32(smem_q + (buf * 2 + s) * C::TILE_BYTES + c * (ROWS * 128)), &tm_q, c * CHUNK, 0, it.t0 + s * a.nt, it.kvh, it.b, qf);
                 ++q_issued;
-                for (int j = 0; j < 2 * it.tiles && ok; ++j) {
+                for (int j = 0; j < 2 * it.n && ok; ++j) {
                     ok = mbar_wait(smem_u32(&bars->empty[st]), ph ^ 1, abort_flag);
                     if (!ok) break;
                     const uint32_t full = smem_u32(&bars->full[st]);
                     mbar_arrive_expect_tx(full, C::TILE_BYTES);
                     // K0, V0, K1, V1, ...; APART: K0, K1, V0, K2, V1, ...
-                    const bool is_v = C::APART ? j > 0 && ((j & 1) == 0 || (j + 1) / 2 == it.tiles) : (j & 1) != 0;
-                    const int tile = !C::APART ? j >> 1 : (j & 1) == 0 ? max(j / 2 - 1, 0) : is_v ? it.tiles - 1 : (j + 1) / 2;
+                    const bool is_v = C::APART ? j > 0 && ((j & 1) == 0 || (j + 1) / 2 == it.n) : (j & 1) != 0;
+                    const int tile = it.j0 + (!C::APART ? j >> 1 : (j & 1) == 0 ? max(j / 2 - 1, 0) : is_v ? it.n - 1 : (j + 1) / 2);
                     for (int c = 0; c < C::CHUNKS; ++c) {
                         const uint32_t dst = smem_u32(smem_st + st * C::TILE_BYTES + c * (KEYS * 128));
                         if (is_v) tma_load_4d(dst, &tm_v, c * CHUNK, tile * KEYS, it.kvh * a.vh, it.b * a.vb, full);
@@ -532,12 +648,12 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
         if constexpr (C::APART) {
             const int s = warp - MMA_WARP;
             uint32_t n_p = 0, n_f = 0;
-            for (Items it(a); it.take(a, lens);) {
-                if (!it.tiles) continue;
+            for (Items<SPLIT> it(a); it.take(a, lens);) {
+                if (!it.n) continue;
                 if (*abort_flag) break;
                 wait_on(&bars->q_full[n_q % C::Q_BUFS], (n_q / C::Q_BUFS) & 1);
                 if (s >= it.streams) {                       // nothing to do but to hand the stages back
-                    for (int j = 0; j < 2 * it.tiles; ++j) {
+                    for (int j = 0; j < 2 * it.n; ++j) {
                         wait_on(&bars->full[st], ph);
                         if (lane == 0) mbar_arrive(smem_u32(&bars->empty[st]));
                         step();
@@ -554,14 +670,14 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                     if (last) commit(&bars->q_empty[n_q % C::Q_BUFS]);
                     step();
                 };
-                scores(it.tiles == 1);
-                for (int j = 0; j < it.tiles; ++j) {
-                    const int valid = min(KEYS, it.len - j * KEYS), steps = (valid + 15) >> 4;
-                    const bool last = j + 1 == it.tiles;
+                scores(it.n == 1);
+                for (int j = 0; j < it.n; ++j) {
+                    const int valid = min(KEYS, it.len - (it.j0 + j) * KEYS), steps = (valid + 15) >> 4;
+                    const bool last = j + 1 == it.n;
                     if (!last) {
                         wait_on(&bars->s_free[s], n_f & 1);
                         ++n_f;
-                        scores(j + 2 == it.tiles);
+                        scores(j + 2 == it.n);
                     }
                     wait_on(&bars->full[st], ph);
                     clear_rows(st, valid, steps);            // (both warps write the same zeros)
@@ -580,19 +696,19 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
             }
         } else {
             uint32_t n_p[2] = {0, 0};
-            for (Items it(a); it.take(a, lens);) {
-                if (!it.tiles) continue;
+            for (Items<SPLIT> it(a); it.take(a, lens);) {
+                if (!it.n) continue;
                 if (*abort_flag) break;
                 wait_on(&bars->q_full[n_q % C::Q_BUFS], (n_q / C::Q_BUFS) & 1);
                 wait_on(&bars->full[st], ph);
                 for (int s = 0; s < it.streams; ++s) issue_qk(s, st);
                 commit(&bars->empty[st]);
-                if (it.tiles == 1) commit(&bars->q_empty[n_q % C::Q_BUFS]);
+                if (it.n == 1) commit(&bars->q_empty[n_q % C::Q_BUFS]);
                 step();
-                for (int j = 0; j < it.tiles; ++j) {
+                for (int j = 0; j < it.n; ++j) {
                     const uint32_t v_st = st;
-                    const int valid = min(KEYS, it.len - j * KEYS), steps = (valid + 15) >> 4;
-                    const bool last = j + 1 == it.tiles;
+                    const int valid = min(KEYS, it.len - (it.j0 + j) * KEYS), steps = (valid + 15) >> 4;
+                    const bool last = j + 1 == it.n;
                     wait_on(&bars->full[st], ph);
                     step();
                     clear_rows(v_st, valid, steps);
@@ -611,7 +727,7 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
                             issue_qk(s, st);
                             if (s + 1 == it.streams) {
                                 commit(&bars->empty[st]);
-                                if (j + 2 == it.tiles) commit(&bars->q_empty[n_q % C::Q_BUFS]);
+                                if (j + 2 == it.n) commit(&bars->q_empty[n_q % C::Q_BUFS]);
                             }
                         }
                         __syncwarp();
@@ -630,6 +746,7 @@ xattn_tc_kernel(const Params a, const __grid_constant__ CUtensorMap tm_q, const 
     }
     tc_fence_before();
     __syncthreads();
+    if (SPLIT) cluster_sync_all();                    // nobody leaves while others read its memory
     if (warp == MMA_WARP) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
@@ -646,15 +763,35 @@ bool encode_rows(CUtensorMap* tm, const XAttnArgs& a, const void* p, const Strid
            encode_map(tm, p, 5, dims, st, box);
 }
 
+// How the items are shared out: as many rounds of whole ones as fill every CTA, and the rest (all, where there are few) divided by keys within
+// clusters.  The fewest tiles in a row, counting what an item (a meeting) costs besides its tiles.
+struct Division { int splits; uint32_t whole, grid; };
+template <int DP> Division divide(uint32_t items, int Tk, int sms) {
+    const int64_t tiles = (Tk + KEYS - 1) / KEYS;
+    Division best{1, items, std::min(items, (uint32_t)sms)};
+    double cost = (double)((items + best.grid - 1) / best.grid) * (double)(tiles + 1);
+    for (int n = 2; n <= MAX_SPLITS && n <= tiles; ++n) {
+        const int held = xa::clusters_held<xattn_tc_kernel<DP, true>>(NUM_THREADS, Cfg<DP>::SMEM, n);
+        if (held < 1) continue;
+        const uint32_t ctas = (uint32_t)(held * n), whole = items / ctas * ctas, left = items - whole;
+        if (left == 0) continue;
+        const double c = (double)(whole / ctas) * (double)(tiles + 1) + (double)((left + held - 1) / held) * ((double)((tiles + n - 1) / n) + MEET_TILES);
+        if (c < cost) { cost = c; best = {n, whole, whole ? ctas : std::min(left, (uint32_t)held) * (uint32_t)n}; }
+    }
+    return best;
+}
+
 template <int DP> cudaError_t launch(Params& p, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& to, int sms, cudaStream_t s) {
-    const cudaError_t e = cc::set_smem_limit<xattn_tc_kernel<DP>>(Cfg<DP>::SMEM);
-    if (e != cudaSuccess) return e;
-    const uint32_t grid = std::min(p.items, (uint32_t)sms), heads = grid / (uint32_t)p.q_items;
+    constexpr int smem = Cfg<DP>::SMEM;
+    const Division d = divide<DP>(p.items, p.Tk, sms);
+    p.splits = d.splits;
+    p.whole = d.whole;
+    const uint32_t grid = d.grid, heads = grid / (uint32_t)p.q_items;
     p.dq = (int)(grid % (uint32_t)p.q_items);
     p.dh = (int)(heads % (uint32_t)p.Hkv);
     p.db = (int)(heads / (uint32_t)p.Hkv);
-    xattn_tc_kernel<DP><<<grid, NUM_THREADS, Cfg<DP>::SMEM, s>>>(p, tq, tk, tv, to);
-    return cudaGetLastError();
+    if (p.splits > 1) return cc::launch_clusters<xattn_tc_kernel<DP, true>>({grid, NUM_THREADS, smem, smem, p.splits}, s, p, tq, tk, tv, to);
+    return cc::launch_clusters<xattn_tc_kernel<DP, false>>({grid, NUM_THREADS, smem, smem, 1}, s, p, tq, tk, tv, to);
 }
 
 }  // namespace
@@ -672,7 +809,8 @@ bool xattn_tc_supported(const XAttnArgs& a) {
 cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s) {
     CUtensorMap tq, tk, tv, to;
     Params p;
-    p.o = a.o; p.lens = a.kv_lens;
+    p.o = (__nv_bfloat16*)a.o; p.o_batch = a.so.batch; p.o_token = a.so.token; p.o_head = a.so.head;
+    p.lens = a.kv_lens;
     p.Tq = a.Tq; p.Tk = a.Tk; p.B = a.B; p.Hkv = a.Hkv; p.g = a.H / a.Hkv; p.D = a.D; p.nt = ROWS / p.g;
     p.q_items = (a.Tq + 2 * p.nt - 1) / (2 * p.nt);
     p.items = (uint32_t)((int64_t)p.q_items * a.Hkv * a.B);          // (rows are at most 2^30)

@@ -41,7 +41,9 @@ SIZES = [  # b, tq, tk, h, hkv, d
     (1, 1, 1, 1, 1, 64), (2, 1, 7, 4, 4, 64), (3, 1, 130, 8, 2, 128), (2, 3, 300, 6, 2, 80), (1, 17, 33, 5, 5, 40), (2, 64, 77, 3, 3, 64),
     (1, 127, 129, 2, 2, 128), (2, 128, 128, 2, 1, 64), (1, 129, 127, 4, 2, 96), (1, 255, 256, 3, 1, 128), (2, 257, 385, 2, 2, 72), (1, 300, 1, 2, 2, 64),
     (1, 513, 640, 2, 1, 32), (1, 1, 2049, 8, 1, 128), (1, 2, 5000, 4, 4, 64), (5, 31, 511, 7, 7, 128), (1, 40, 700, 30, 6, 64), (1, 9, 100, 16, 1, 128),
-    (1, 130, 260, 3, 3, 256), (2, 5, 50, 2, 2, 1), (1, 16, 300, 2, 2, 128), (2, 1, 1000, 10, 1, 64), (1, 11, 77, 1, 1, 40), (1, 4, 500, 8, 4, 96), (3, 2, 4100, 12, 2, 128), (1, 8, 17, 2, 2, 72), (2, 1, 900, 3, 1, 256), (1, 19, 21, 2, 1, 7), (1, 70, 200, 2, 2, 160), (1, 20, 90, 1, 1, 255)]
+    (1, 130, 260, 3, 3, 256), (2, 5, 50, 2, 2, 1), (1, 16, 300, 2, 2, 128), (2, 1, 1000, 10, 1, 64), (1, 11, 77, 1, 1, 40), (1, 4, 500, 8, 4, 96), (3, 2, 4100, 12, 2, 128), (1, 8, 17, 2, 2, 72), (2, 1, 900, 3, 1, 256), (1, 19, 21, 2, 1, 7), (1, 70, 200, 2, 2, 160), (1, 20, 90, 1, 1, 255),
+    # few items: their keys divided among a cluster; many: whole ones and divided ones in one call (148 SMs)
+    (1, 300, 5000, 2, 2, 128), (1, 130, 3001, 3, 1, 64), (2, 700, 2000, 5, 5, 128), (1, 17, 9000, 1, 1, 64), (1, 50, 4000, 12, 2, 72), (1, 5400, 1100, 8, 8, 64), (1, 5400, 700, 8, 8, 128)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -51,7 +53,8 @@ def test_full_lengths(vd, dtype, size):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("size", [(4, 1, 200, 4, 2, 64), (4, 33, 300, 2, 2, 128), (5, 140, 270, 3, 1, 80), (4, 300, 129, 2, 2, 64), (4, 2, 40, 2, 2, 7)],
+@pytest.mark.parametrize("size", [(4, 1, 200, 4, 2, 64), (4, 33, 300, 2, 2, 128), (5, 140, 270, 3, 1, 80), (4, 300, 129, 2, 2, 64), (4, 2, 40, 2, 2, 7), (5, 100, 3000, 2, 2, 128),
+                                  (5, 300, 2500, 2, 1, 64), (5, 5, 3000, 4, 2, 64), (5, 40, 3000, 6, 2, 80)],
                          ids=lambda s: "x".join(map(str, s)))
 def test_ragged_lengths_with_garbage_behind_them(vd, dtype, size):
     """One row without keys, one of one key, one clamped from above, the others ragged; NaN, infinities and the type's lowest value behind each
@@ -59,7 +62,7 @@ def test_ragged_lengths_with_garbage_behind_them(vd, dtype, size):
     import torch
     b, _, tk = size[:3]
     q, k, v = make(dtype, *size, seed=1)
-    lens = [0, 1, tk + 9, (2 * tk) // 3 + 1, tk // 2][:b]
+    lens = [0, 1, tk + 9, (2 * tk) // 3 + 1, tk // 12][:b]
     clean = [x.clone() for x in (k, v)]
     for i, n in enumerate(lens):
         n = min(n, tk)
@@ -168,7 +171,7 @@ def test_nan_and_infinity_in_what_counts(vd, dtype, tq):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("size", [(1, 300, 700, 4, 2, 64), (2, 1, 3000, 8, 2, 128), (2, 6, 90, 4, 2, 64)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("size", [(1, 300, 700, 4, 2, 64), (2, 1, 3000, 8, 2, 128), (2, 6, 90, 4, 2, 64), (1, 150, 6000, 2, 2, 128), (2, 1350, 500, 30, 30, 64), (1, 3000, 1500, 16, 16, 128)], ids=lambda s: "x".join(map(str, s)))
 def test_same_bits_each_time_on_any_stream_and_in_a_graph(vd, dtype, size):
     import torch
     q, k, v = make(dtype, *size, seed=7)
