@@ -499,6 +499,29 @@ def op_attention(qkv, channels: int, scale: float, impl=VD_IMPL_AUTO):
 
 
 # ---- operators of a latent world model's transformer block (include/vd_block.h) -----------------
+# A call's checks and its descriptor follow from the tensors' types, shapes, strides and devices alone, and are kept by these:
+# a token's operators are over on the device before Python has looked at their arguments once more.
+_descriptors = {}
+
+
+def _described(key, describe, *args):
+    desc = _descriptors.get(key)
+    if desc is None:
+        desc = describe(*args)
+        if len(_descriptors) >= 1024:
+            _descriptors.clear()
+        _descriptors[key] = desc
+    return desc
+
+
+def _sig(t):
+    return None if t is None else (t.dtype, t.shape, t.stride(), t.get_device())
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
 def _refuse(msg: str):
     raise VdError(VD_ERR_INVALID_ARG, msg)
 
@@ -512,16 +535,6 @@ def _block_dtype(t, name: str) -> int:
     return VD_F32
 
 
-def _launch(device, call):
-    """call(stream) with the tensors' device current, on its current stream."""
-    import torch
-    if device.index == torch.cuda.current_device():
-        _check(call(torch.cuda.current_stream().cuda_stream))
-    else:
-        with torch.cuda.device(device):
-            _check(call(torch.cuda.current_stream().cuda_stream))
-
-
 def _on_device(ref, **others):
     if not ref.is_cuda:
         _refuse("tensors must be on a CUDA device")
@@ -530,10 +543,27 @@ def _on_device(ref, **others):
             _refuse(f"{name} is on {t.device}, not on {ref.device}")
 
 
-def op_cross_attention(q, k, v, kv_lens=None, scale=None, out=None, impl=VD_XATTN_AUTO):
-    """Attention of q [B,Tq,H,D] to k and v [B,Tk,Hkv,D] (H a multiple of Hkv; float32 or bfloat16; slices and expanded tensors
-    are taken as they are, channels side by side) -> [B,Tq,H,D].  kv_lens: int32 [B], the keys of each item, or None for
-    all Tk; a row without keys is zeros.  scale: D ** -0.5 if None.  Gradients are not taken."""
+def _current_stream(device: int) -> int:
+    """The address of a device's current stream: a stream object costs three microseconds, a third of a call."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+def _launch(t, call, *args):
+    """call(*args, stream) with t's device current, on its current stream."""
+    import torch
+    device = t.get_device()
+    if device == torch.cuda.current_device():
+        status = call(*args, _current_stream(device))
+    else:
+        with torch.cuda.device(device):
+            status = call(*args, _current_stream(device))
+    if status != VD_OK:
+        _check(status)
+
+
+def _describe_cross_attention(q, k, v, kv_lens, scale, out, impl):
     import torch
     if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape:
         _refuse("q [B,Tq,H,D], k and v [B,Tk,Hkv,D]")
@@ -541,9 +571,7 @@ def op_cross_attention(q, k, v, kv_lens=None, scale=None, out=None, impl=VD_XATT
     kb, tk, hkv, kd = k.shape
     if kb != b or kd != d:
         _refuse("q, k and v disagree in batch or head size")
-    if out is None:
-        out = torch.empty((b, tq, h, d), dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape:
+    if out.shape != q.shape:
         _refuse("out must have q's shape")
     if not q.dtype == k.dtype == v.dtype == out.dtype:
         _refuse("q, k, v and out must have one type")
@@ -553,10 +581,20 @@ def op_cross_attention(q, k, v, kv_lens=None, scale=None, out=None, impl=VD_XATT
     sq, sk, sv, so = q.stride(), k.stride(), v.stride(), out.stride()
     if d > 1 and not sq[3] == sk[3] == sv[3] == so[3] == 1:
         _refuse("the channels of a head must lie side by side")
-    desc = VdXattnDesc(ctypes.sizeof(VdXattnDesc), _block_dtype(q, "q"), b, tq, tk, h, hkv, d, impl, d ** -0.5 if scale is None else scale,
+    return VdXattnDesc(ctypes.sizeof(VdXattnDesc), _block_dtype(q, "q"), b, tq, tk, h, hkv, d, impl, d ** -0.5 if scale is None else scale,
                        sq[0], sq[1], sq[2], sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], so[0], so[1], so[2])
-    lens = None if kv_lens is None else kv_lens.data_ptr()
-    _launch(q.device, lambda stream: lib().vd_op_cross_attention(byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), lens, out.data_ptr(), stream))
+
+
+def op_cross_attention(q, k, v, kv_lens=None, scale=None, out=None, impl=VD_XATTN_AUTO):
+    """Attention of q [B,Tq,H,D] to k and v [B,Tk,Hkv,D] (H a multiple of Hkv; float32 or bfloat16; slices and expanded tensors
+    are taken as they are, channels side by side) -> [B,Tq,H,D].  kv_lens: int32 [B], the keys of each item, or None for
+    all Tk; a row without keys is zeros.  scale: D ** -0.5 if None.  Gradients are not taken."""
+    import torch
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    desc = _described(("xattn", scale, impl, _sig(q), _sig(k), _sig(v), _sig(kv_lens), _sig(out)), _describe_cross_attention,
+                      q, k, v, kv_lens, scale, out, impl)
+    _launch(q, lib().vd_op_cross_attention, byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(kv_lens), out.data_ptr())
     return out
 
 
@@ -574,11 +612,7 @@ def rotary_frequencies(rotary_dim: int, base: float = 10000.0, *, axis_pairs=Non
     return torch.tensor(out[:rotary_dim // 2], dtype=torch.float64)
 
 
-def op_rotary(x, freqs, positions=None, *, layout="half", axis_pairs=None, amplitude: float = 1.0, first_position: int = 0, out=None):
-    """Rotary positions of x [B,T,H,D] (float32 or bfloat16; q and k side by side in one tensor take one call): the first
-    2 * len(freqs) channels of each head turn, the others are copied.  freqs: float64 [R/2] on the device, turns per position
-    (rotary_frequencies).  positions: int32 [B,T] or [B,T,axes] (expanded over the batch is fine), or None: first_position, + 1, ...
-    axis_pairs: the pairs of each axis.  layout: "half" or "interleaved".  out may be x."""
+def _describe_rotary(x, freqs, positions, layout, axis_pairs, amplitude, first_position, out):
     import torch
     if x.dim() != 4:
         _refuse("x [B,T,H,D]")
@@ -586,14 +620,12 @@ def op_rotary(x, freqs, positions=None, *, layout="half", axis_pairs=None, ampli
     if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
         _refuse("freqs must be a contiguous float64 tensor [R/2]")
     n = freqs.shape[0]
-    pairs = (n,) if axis_pairs is None else tuple(axis_pairs)
+    pairs = (n,) if axis_pairs is None else axis_pairs
     if not 1 <= len(pairs) <= VD_ROTARY_MAX_AXES:
         _refuse("bad number of axes")
     if layout not in ("half", "interleaved"):
         _refuse("layout: half or interleaved")
-    if out is None:
-        out = torch.empty((b, t, h, d), dtype=x.dtype, device=x.device)
-    elif out.shape != x.shape or out.dtype != x.dtype:
+    if out.shape != x.shape or out.dtype != x.dtype:
         _refuse("out must have x's shape and type")
     _on_device(x, freqs=freqs, positions=positions, out=out)
     pb = pt = 0
@@ -606,20 +638,28 @@ def op_rotary(x, freqs, positions=None, *, layout="half", axis_pairs=None, ampli
     sx, sy = x.stride(), out.stride()
     if d > 1 and not sx[3] == sy[3] == 1:
         _refuse("the channels of a head must lie side by side")
-    desc = VdRotaryDesc(ctypes.sizeof(VdRotaryDesc), _block_dtype(x, "x"), b, t, h, d, 2 * n, VD_ROTARY_INTERLEAVED if layout == "interleaved" else VD_ROTARY_HALF,
+    return VdRotaryDesc(ctypes.sizeof(VdRotaryDesc), _block_dtype(x, "x"), b, t, h, d, 2 * n, VD_ROTARY_INTERLEAVED if layout == "interleaved" else VD_ROTARY_HALF,
                         len(pairs), (c_int32 * VD_ROTARY_MAX_AXES)(*pairs), amplitude, sx[0], sx[1], sx[2], sy[0], sy[1], sy[2], pb, pt,
                         first_position)
-    at = None if positions is None else positions.data_ptr()
-    _launch(x.device, lambda stream: lib().vd_op_rotary(byref(desc), x.data_ptr(), at, freqs.data_ptr(), out.data_ptr(), stream))
+
+
+def op_rotary(x, freqs, positions=None, *, layout="half", axis_pairs=None, amplitude: float = 1.0, first_position: int = 0, out=None):
+    """Rotary positions of x [B,T,H,D] (float32 or bfloat16; q and k side by side in one tensor take one call): the first
+    2 * len(freqs) channels of each head turn, the others are copied.  freqs: float64 [R/2] on the device, turns per position
+    (rotary_frequencies).  positions: int32 [B,T] or [B,T,axes] (expanded over the batch is fine), or None: first_position, + 1, ...
+    axis_pairs: the pairs of each axis.  layout: "half" or "interleaved".  out may be x."""
+    import torch
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if axis_pairs is not None:
+        axis_pairs = tuple(axis_pairs)
+    desc = _described(("rotary", layout, axis_pairs, amplitude, first_position, _sig(x), _sig(freqs), _sig(positions), _sig(out)), _describe_rotary,
+                      x, freqs, positions, layout, axis_pairs, amplitude, first_position, out)
+    _launch(x, lib().vd_op_rotary, byref(desc), x.data_ptr(), _ptr(positions), freqs.data_ptr(), out.data_ptr())
     return out
 
 
-def op_gate_norm(x, h=None, *, gate=None, scale=None, shift=None, kind="layer", eps: float = 1e-6, weight=None, bias=None, post_norm=False,
-                 post_weight=None, residual_scale: float = 1.0, mod_tokens=None, x_out=None, y=None, want_x=True, want_y=True):
-    """r = x + residual_scale * gate * u, u = h or norm(h) * post_weight, and y = (norm(r) * weight + bias) * (1 + scale) + shift, of tokens
-    [B,T,C] -> (r in x's type, y in h's type, or x's without h).  gate, scale, shift: [B,M,C] of one type, a row for every
-    mod_tokens tokens (M = ceil(T / mod_tokens); None: all of an item's).  weight, bias, post_weight: float32 [C].  kind: "layer" or
-    "rms".  x_out may be x, y may be h; want_x, want_y: False leaves that output out (None)."""
+def _describe_gate_norm(x, h, gate, scale, shift, kind, eps, weight, bias, post_norm, post_weight, residual_scale, mod_tokens, x_out, y):
     import torch
     if x.dim() != 3 or (h is not None and h.shape != x.shape):
         _refuse("x and h [B,T,C]")
@@ -629,8 +669,6 @@ def op_gate_norm(x, h=None, *, gate=None, scale=None, shift=None, kind="layer", 
     mod_tokens = max(t, 1) if mod_tokens is None else mod_tokens
     if mod_tokens < 1:
         _refuse("mod_tokens must be positive")
-    x_out = (torch.empty((b, t, c), dtype=x.dtype, device=x.device) if x_out is None else x_out) if want_x else None
-    y = (torch.empty((b, t, c), dtype=x.dtype if h is None else h.dtype, device=x.device) if y is None else y) if want_y else None
     for name, o in (("x_out", x_out), ("y", y)):
         if o is not None and o.shape != x.shape:
             _refuse(f"{name} must have x's shape")
@@ -662,10 +700,23 @@ def op_gate_norm(x, h=None, *, gate=None, scale=None, shift=None, kind="layer", 
         rows += [r.stride(0), r.stride(1)]
     xd = _block_dtype(x, "x")
     mods = next((m for m in (gate, scale, shift) if m is not None), None)
-    desc = VdGateNormDesc(ctypes.sizeof(VdGateNormDesc), b, t, c, xd, xd if h is None else _block_dtype(h, "h"), xd if y is None else _block_dtype(y, "y"),
+    return VdGateNormDesc(ctypes.sizeof(VdGateNormDesc), b, t, c, xd, xd if h is None else _block_dtype(h, "h"), xd if y is None else _block_dtype(y, "y"),
                           VD_F32 if mods is None else _block_dtype(mods, "gate, scale and shift"), VD_NORM_RMS if kind == "rms" else VD_NORM_LAYER,
                           int(post_norm), mod_tokens, eps, residual_scale, *rows, *strides)
-    p = lambda v: None if v is None else v.data_ptr()
-    _launch(x.device, lambda stream: lib().vd_op_gate_norm(byref(desc), p(x), p(h), p(post_weight), p(gate), p(x_out), p(weight), p(bias),
-                                                           p(scale), p(shift), p(y), stream))
+
+
+def op_gate_norm(x, h=None, *, gate=None, scale=None, shift=None, kind="layer", eps: float = 1e-6, weight=None, bias=None, post_norm=False,
+                 post_weight=None, residual_scale: float = 1.0, mod_tokens=None, x_out=None, y=None, want_x=True, want_y=True):
+    """r = x + residual_scale * gate * u, u = h or norm(h) * post_weight, and y = (norm(r) * weight + bias) * (1 + scale) + shift, of tokens
+    [B,T,C] -> (r in x's type, y in h's type, or x's without h).  gate, scale, shift: [B,M,C] of one type, a row for every
+    mod_tokens tokens (M = ceil(T / mod_tokens); None: all of an item's).  weight, bias, post_weight: float32 [C].  kind: "layer" or
+    "rms".  x_out may be x, y may be h; want_x, want_y: False leaves that output out (None)."""
+    import torch
+    x_out = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if x_out is None else x_out) if want_x else None
+    y = (torch.empty(x.shape, dtype=x.dtype if h is None else h.dtype, device=x.device) if y is None else y) if want_y else None
+    desc = _described(("norm", kind, eps, post_norm, residual_scale, mod_tokens, _sig(x), _sig(h), _sig(gate), _sig(scale), _sig(shift), _sig(weight), _sig(bias),
+                       _sig(post_weight), _sig(x_out), _sig(y)), _describe_gate_norm,
+                      x, h, gate, scale, shift, kind, eps, weight, bias, post_norm, post_weight, residual_scale, mod_tokens, x_out, y)
+    _launch(x, lib().vd_op_gate_norm, byref(desc), x.data_ptr(), _ptr(h), _ptr(post_weight), _ptr(gate), _ptr(x_out), _ptr(weight), _ptr(bias),
+            _ptr(scale), _ptr(shift), _ptr(y))
     return x_out, y

@@ -31,7 +31,7 @@ constexpr int HALF = KEYS / 2;                               // keys of P that g
 constexpr int SOFTMAX_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, NUM_THREADS = 352;     // MMA_WARP + s issues for tile s
 constexpr int MAX_LENS = 128;                                // lengths that are kept in shared memory
 constexpr int MAX_SPLITS = xa::MAX_SPLITS;
-constexpr double MEET_TILES = 4.0;                           // what a meeting costs, in tiles
+constexpr double MEET_TILES = 8.0;                           // what a meeting costs, in tiles
 constexpr float RESCALE_THRESHOLD = 8.0f;                    // log2 units: accumulators may grow by 2^8
 
 template <int DP> struct Cfg {
@@ -411,11 +411,14 @@ __device__ __noinline__ void meet(const Params& a, const Items<true>& it, Bars* 
             const int r = i / PIECES, piece = i % PIECES, tt = r / a.g, t = it.t0 + s * a.nt + tt, d = round * COLS + piece * 4;
             if (tt >= a.nt || t >= a.Tq || d >= a.D) continue;
             const uint32_t at = smem_u32(show + r * (COLS * 4) + ((piece ^ (r & (PIECES - 1))) << 4)), at_ml = smem_u32(ml + r);
+            // (loads of other CTAs' memory take a thousand cycles: some at a time, but not so many that the call's registers crowd the softmax's)
             float top = -INFINITY;
+#pragma unroll 4
             for (int k = 0; k < a.splits; ++k) top = fmaxf(top, ld_cluster2(map_to_cta(at_ml, (uint32_t)k)).x);
             const float ref = top == -INFINITY ? 0.f : top;
             float l = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
             for (int k = 0; k < a.splits; ++k) {
                 const float2 w = ld_cluster2(map_to_cta(at_ml, (uint32_t)k));
                 const float4 v = ld_cluster4(map_to_cta(at, (uint32_t)k));
