@@ -126,11 +126,17 @@ __global__ void __launch_bounds__(MAX_THREADS) rotary_kernel(const RotaryArgs a)
 template <typename T> cudaError_t launch_vec(const RotaryArgs& a, cudaStream_t s) {
     constexpr int V = 16 / sizeof(T);
     const int units = (a.interleaved ? a.R / V : a.R / 2 / V) + (a.D - a.R) / V;
-    const int heads = a.H < MAX_THREADS / units ? a.H : MAX_THREADS / units;
     const int64_t tokens = (int64_t)a.B * a.T;
-    int per = MAX_THREADS / (units * heads);                 // small tokens share a block, as long as the blocks cover the GPU
+    // A thread takes HEADS heads where there are tokens enough, and small tokens share a block of 128 threads: many small blocks, each with
+    // its loads under way, hide one another's tables (us: 21600 x 60 heads of 64 two heads a thread 82, four 56, eight 55; 8192 x 40 of 128
+    // 50, 31, 33; three axes, interleaved, and one, halves).
+    const int each = tokens >= 8 * 148 ? HEADS : 1;
+    int heads = (a.H + each - 1) / each;
+    if (heads > MAX_THREADS / units) heads = MAX_THREADS / units;
+    int per = 128 / (units * heads);
     while (per > 1 && (tokens + per - 1) / per < 4 * 148) --per;
     if (per > 16) per = 16;
+    if (per < 1) per = 1;
     const dim3 grid((unsigned)((tokens + per - 1) / per)), block(units, heads, per);
     const size_t smem = (size_t)per * (a.R / 2) * sizeof(float2);
     if (a.interleaved) rotary_vec_kernel<T, false><<<grid, block, smem, s>>>(a);

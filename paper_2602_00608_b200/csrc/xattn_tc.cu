@@ -44,7 +44,7 @@ template <int DP> struct Cfg {
     static constexpr uint32_t P_COL = APART ? 384 : 0, P_STEP = APART ? 64 : 128;
     // every so many pairs of exponentials one on the FMA pipes; 0: none.  (They take five instructions for one, and where the products are
     // short the issue slots are what is short.)
-    static constexpr int POLY = APART ? 0 : 8;
+    static constexpr int POLY = APART ? 0 : 16;
     static constexpr int MMA_WARPS = APART ? 2 : 1;
     static constexpr int SMEM = (Q_BUFS * 2 + 2 + STAGES) * TILE_BYTES + 2 * ROWS * 8 + MAX_LENS * 4 + 320;     // Q, O on its way out, K and V; (reference, sum) of the rows
 };
