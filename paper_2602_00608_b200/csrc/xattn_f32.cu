@@ -1,11 +1,13 @@
 // Attention to states of another length in single precision, on the FP32 pipes (no operand or sum in fewer bits; the tensor core
 // drops what falls off a running sum, and one of several hundred keys shows it).  A CTA of 128 threads takes 64 rows of a key head
 // (a row: a token and one of the heads that share it) and walks blocks of 16 NJ keys; two CTAs share an SM, so that one computes
-// while the other exchanges.  A thread holds 8 rows x NJ keys of the scores, as pairs along the channels, so that both operands are
-// pairs as they lie in memory (fma.rn.f32x2), and 8 rows x NC channels of the output, as pairs of rows.  The keys of a thread are 16
-// apart and a key's row in shared memory is an odd multiple of 16 bytes: no bank conflicts.  P goes through shared memory, its
-// 16-byte pieces exchanged by key.  k, v and q come by cp.async, k and v one step ahead of their use.
-// Where there are few rows a cluster divides the keys (xattn_meet.cuh).
+// while the other exchanges.  All products are fma.rn.f32x2 on pairs that lie in shared memory as they are needed: a move that makes a
+// pair of one number runs on the same pipes (they cost a quarter of the time).
+//   scores   8 rows x NJ keys of a thread, pairs along the channels.  Its keys are 16 apart and a key's row is an odd multiple of 16
+//            bytes long: no bank conflicts
+//   output   4 rows x DM / 8 channels of a thread, pairs of channels; P is stored as pairs of equal numbers, its 16-byte pieces exchanged by
+//            key.  A warp's 16 rows are its own in either shape, so P needs no barrier
+// k, v and q come by cp.async, k and v one step ahead of their use.  Where there are few rows a cluster divides the keys (xattn_meet.cuh).
 #include "block_ops.h"
 #include "xattn_meet.cuh"
 
@@ -17,42 +19,45 @@ using namespace xa;
 
 constexpr int ROWS = 64, THREADS = 128;
 
-template <int NC> struct Cfg {                               // NC: output channels of a thread
-    static constexpr int DM = NC * 16, NJ = NC > 6 ? 3 : 4, KEYS = NJ * 16;
-    static constexpr int VEC = NC % 4 == 0 ? 4 : NC % 2 == 0 ? 2 : 1;
-    // Q [64][DM], K [KEYS][DM + 4], V [KEYS][DM], P [KEYS][64]
-    static constexpr int Q_AT = 0, K_AT = ROWS * DM, V_AT = K_AT + KEYS * (DM + 4), P_AT = V_AT + KEYS * DM, END = P_AT + KEYS * ROWS;
+template <int DM_> struct Cfg {                              // DM: channels that are held, a multiple of 16
+    static constexpr int DM = DM_, NJ = DM > 96 ? 3 : 4, KEYS = NJ * 16;
+    static constexpr int NC = DM / 8, QUADS = NC / 4, REST = NC % 4;     // channels of a thread's output: QUADS times four, 32 apart, and two more
+    // Q [64][DM], K [KEYS][DM + 4], V [KEYS][DM], P [KEYS][64] pairs
+    static constexpr int Q_AT = 0, K_AT = ROWS * DM, V_AT = K_AT + KEYS * (DM + 4), P_AT = V_AT + KEYS * DM, END = P_AT + KEYS * ROWS * 2;
     static constexpr int SMEM = END * 4;
-    static_assert((DM + 4) % 8 == 4, "an odd multiple of 16 bytes");
+    static_assert((DM + 4) % 8 == 4 && (REST == 0 || REST == 2), "an odd multiple of 16 bytes; whole pairs");
     static_assert(2 * (SMEM + 1024) <= 228 * 1024, "two CTAs share an SM");
     static_assert(ROWS * (DM + 2) <= END, "the meeting's memory lies over the others");
 };
 
-template <int NC>
+template <int DM>
 __global__ void __launch_bounds__(THREADS, 2) xattn_f32_kernel(const RowParams p) {
-    using C = Cfg<NC>;
-    constexpr int DM = C::DM, NJ = C::NJ, KEYS = C::KEYS, KS = DM + 4;
+    using C = Cfg<DM>;
+    constexpr int NJ = C::NJ, KEYS = C::KEYS, KS = DM + 4, NC = C::NC;
     extern __shared__ __align__(16) float smem[];
     float *s_q = smem + C::Q_AT, *s_k = smem + C::K_AT, *s_v = smem + C::V_AT, *s_p = smem + C::P_AT;
     const XAttnArgs& a = p.a;
-    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    const int tid = threadIdx.x, lane = tid & 31, tx = tid & 15, ty = tid >> 4, cx = tid & 7, ry = tid >> 3;     // scores: rows 8 ty, keys tx; output: rows 4 ry
     const int split = p.splits > 1 ? (int)cluster_ctarank() : 0;
     const Work w = work_of<ROWS>(p);
     const int tiles = (w.len + KEYS - 1) / KEYS, mine = tiles > split ? (tiles - split + p.splits - 1) / p.splits : 0;
     const int chunks = a.D / 4, lc = tid & 7, lr = tid >> 3; // loads: eight threads per key or row
-    const float* k = (const float*)a.k + w.b * a.sk.batch + w.kvh * a.sk.head;
-    const float* v = (const float*)a.v + w.b * a.sv.batch + w.kvh * a.sv.head;
-    // zeros where there are no channels, rows or keys (0 * NaN is NaN)
+    const float* k = (const float*)a.k + w.b * a.sk.batch + w.kvh * a.sk.head + lc * 4;
+    const float* v = (const float*)a.v + w.b * a.sv.batch + w.kvh * a.sv.head + lc * 4;
+    constexpr int CHUNKS = (DM / 4 + 7) / 8;                 // of a thread's part of a key
+    // zeros where there are no channels or keys (0 * NaN is NaN)
     auto load = [&](float* dst, int stride, const float* src, int64_t token, int key0) {
+        const uint32_t at = smem_u32(dst + lr * stride + lc * 4);
+        const float* row = src + (key0 + lr) * token;
 #pragma unroll
-        for (int r = 0; r < KEYS; r += 16) {
-            const int key = key0 + r + lr;
-            const bool here = key < w.len;
-            const float* row = src + (here ? key : 0) * token;
-            for (int c = lc; c < DM / 4; c += 8) {
-                const bool in = here && c < chunks;
-                cp_async16(smem_u32(dst + (r + lr) * stride + c * 4), in ? row + c * 4 : src, in ? 16u : 0u);
-            }
+        for (int r = 0; r < KEYS; r += 16, row += 16 * token) {
+            const bool here = key0 + r + lr < w.len;
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+                if (DM % 32 == 0 || c + 1 < CHUNKS || lc + 8 * c < DM / 4) {
+                    const bool in = here && lc + 8 * c < chunks;
+                    cp_async16(at + (uint32_t)(r * stride + c * 32) * 4u, in ? row + c * 32 : src, in ? 16u : 0u);
+                }
         }
     };
     for (int r = lr; r < ROWS; r += 16) {
@@ -68,12 +73,12 @@ __global__ void __launch_bounds__(THREADS, 2) xattn_f32_kernel(const RowParams p
     if (mine) load(s_v, DM, v, a.sv.token, split * KEYS);
     cp_async_commit();
 
-    unsigned long long o[4][NC];                             // rows 8 ty + 2i, + 1
+    unsigned long long o[4][NC / 2];                         // rows 4 ry + i
     float m_ref[8], l[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int u = 0; u < NC; ++u) o[i][u] = 0ull;
+        for (int u = 0; u < NC / 2; ++u) o[i][u] = 0ull;
 #pragma unroll
     for (int i = 0; i < 8; ++i) { m_ref[i] = -INFINITY; l[i] = 0.f; }
 
@@ -110,15 +115,19 @@ __global__ void __launch_bounds__(THREADS, 2) xattn_f32_kernel(const RowParams p
         __syncthreads();                                     // K has been read
         if (t + 1 < mine) load(s_k, KS, k, a.sk.token, next);
         cp_async_commit();
+        if (key0 + KEYS > w.len)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+                if (key0 + tx + 16 * j >= w.len)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[i][j] = -INFINITY;
         bool grow = false;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const bool here = key0 + tx + 16 * j < w.len;
+        for (int i = 0; i < 8; ++i) {
+            float top = s[i][0];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (!here) s[i][j] = -INFINITY;
-                grow = grow || s[i][j] > m_ref[i] + RESCALE_THRESHOLD;
-            }
+            for (int j = 1; j < NJ; ++j) top = fmaxf(top, s[i][j]);
+            grow = grow || top > m_ref[i] + RESCALE_THRESHOLD;
         }
         if (__any_sync(0xffffffffu, grow)) {                 // (a row's 16 threads sit in one half of a warp)
             float f[8];
@@ -134,9 +143,12 @@ __global__ void __launch_bounds__(THREADS, 2) xattn_f32_kernel(const RowParams p
                 l[i] *= f[i];
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i) {                    // row 4 ry + i: the factor is with lane 16 (ry & 2) / 2, number 4 (ry & 1) + i
+                const float lo = __shfl_sync(0xffffffffu, f[i], (lane >> 4) << 4), hi = __shfl_sync(0xffffffffu, f[i + 4], (lane >> 4) << 4);
+                const float g = ry & 1 ? hi : lo;
 #pragma unroll
-                for (int u = 0; u < NC; ++u) o[i][u] = fmaf2(o[i][u], pack2(f[2 * i], f[2 * i + 1]), 0ull);
+                for (int u = 0; u < NC / 2; ++u) o[i][u] = fmaf2(o[i][u], pack2(g, g), 0ull);
+            }
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -148,35 +160,36 @@ __global__ void __launch_bounds__(THREADS, 2) xattn_f32_kernel(const RowParams p
             }
         }
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {                       // pieces of four rows, exchanged by key
-            float* row = s_p + (tx + 16 * j) * ROWS;
-            *(float4*)(row + (((ty * 2) ^ tx) << 2)) = make_float4(s[0][j], s[1][j], s[2][j], s[3][j]);
-            *(float4*)(row + (((ty * 2 + 1) ^ tx) << 2)) = make_float4(s[4][j], s[5][j], s[6][j], s[7][j]);
+        for (int j = 0; j < NJ; ++j) {                       // pieces of two rows, exchanged by key
+            float* row = s_p + (tx + 16 * j) * (ROWS * 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(float4*)(row + (((ty * 4 + i) ^ (tx & 7)) << 2)) = make_float4(s[2 * i][j], s[2 * i][j], s[2 * i + 1][j], s[2 * i + 1][j]);
         }
         asm volatile("cp.async.wait_group 1;" ::: "memory"); // V of this block
         __syncthreads();
-#pragma unroll 4
+#pragma unroll 8
         for (int key = 0; key < KEYS; ++key) {
-            const float* row = s_p + key * ROWS;
-            const ulonglong2 p0 = *(const ulonglong2*)(row + (((ty * 2) ^ (key & 15)) << 2)), p1 = *(const ulonglong2*)(row + (((ty * 2 + 1) ^ (key & 15)) << 2));
-            float vv[NC];
+            // (this warp's two pieces lie side by side, the other way round where the key is odd)
+            const float* row = s_p + key * (ROWS * 2) + (((ry * 2) ^ (key & 6)) << 2);
+            const ulonglong2 pa = *(const ulonglong2*)row, pb = *(const ulonglong2*)(row + 4), p0 = key & 1 ? pb : pa, p1 = key & 1 ? pa : pb;
+            unsigned long long vv[NC / 2];
+            const float* at = s_v + key * DM;
 #pragma unroll
-            for (int u = 0; u < NC; u += C::VEC) {
-                const float* at = s_v + key * DM + (u / C::VEC) * 16 * C::VEC + tx * C::VEC;
-                if constexpr (C::VEC == 4) { const float4 x = *(const float4*)at; vv[u] = x.x; vv[u + 1] = x.y; vv[u + 2] = x.z; vv[u + 3] = x.w; }
-                else if constexpr (C::VEC == 2) { const float2 x = *(const float2*)at; vv[u] = x.x; vv[u + 1] = x.y; }
-                else vv[u] = *at;
+            for (int q = 0; q < C::QUADS; ++q) {
+                const ulonglong2 x = *(const ulonglong2*)(at + q * 32 + cx * 4);
+                vv[2 * q] = x.x; vv[2 * q + 1] = x.y;
             }
+            if (C::REST) vv[NC / 2 - 1] = *(const unsigned long long*)(at + C::QUADS * 32 + cx * 2);
 #pragma unroll
-            for (int u = 0; u < NC; ++u) {
-                const unsigned long long x = pack2(vv[u], vv[u]);
-                o[0][u] = fmaf2(p0.x, x, o[0][u]);
-                o[1][u] = fmaf2(p0.y, x, o[1][u]);
-                o[2][u] = fmaf2(p1.x, x, o[2][u]);
-                o[3][u] = fmaf2(p1.y, x, o[3][u]);
+            for (int u = 0; u < NC / 2; ++u) {
+                o[0][u] = fmaf2(p0.x, vv[u], o[0][u]);
+                o[1][u] = fmaf2(p0.y, vv[u], o[1][u]);
+                o[2][u] = fmaf2(p1.x, vv[u], o[2][u]);
+                o[3][u] = fmaf2(p1.y, vv[u], o[3][u]);
             }
         }
-        __syncthreads();                                     // V and P have been read
+        __syncthreads();                                     // V has been read (and P, by its warp)
         if (t + 1 < mine) load(s_v, DM, v, a.sv.token, next);
         cp_async_commit();
     }
@@ -187,27 +200,27 @@ __global__ void __launch_bounds__(THREADS, 2) xattn_f32_kernel(const RowParams p
         for (int x = 1; x < 16; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
     float2* om = (float2*)(smem + ROWS * DM);
     if (p.splits > 1) __syncthreads();                       // the meeting's memory lies over the stages
+    float ll[4];                                             // of rows 4 ry + i, like the factors above
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = ty * 8 + i;
-        if (p.splits > 1) {
-            if (tx == 0) om[r] = make_float2(m_ref[i], l[i]);
+    for (int i = 0; i < 4; ++i) {
+        const float lo = __shfl_sync(0xffffffffu, l[i], (lane >> 4) << 4), hi = __shfl_sync(0xffffffffu, l[i + 4], (lane >> 4) << 4);
+        ll[i] = ry & 1 ? hi : lo;
+    }
+    if (p.splits > 1 && tx == 0)
 #pragma unroll
-            for (int u = 0; u < NC; ++u) {
-                float lo, hi;
-                unpack2(o[i >> 1][u], lo, hi);
-                smem[r * DM + (u / C::VEC) * 16 * C::VEC + tx * C::VEC + u % C::VEC] = i & 1 ? hi : lo;
-            }
-        } else if (r < w.rows) {
-            float* out = (float*)a.o + w.at(p, a.so, r);
-            const float inv = w.len ? 1.f / l[i] : 0.f;
+        for (int i = 0; i < 8; ++i) om[ty * 8 + i] = make_float2(m_ref[i], l[i]);
 #pragma unroll
-            for (int u = 0; u < NC; ++u) {
-                const int d = (u / C::VEC) * 16 * C::VEC + tx * C::VEC + u % C::VEC;
-                float lo, hi;
-                unpack2(o[i >> 1][u], lo, hi);
-                if (d < a.D) out[d] = (i & 1 ? hi : lo) * inv;
-            }
+    for (int i = 0; i < 4; ++i) {
+        const int r = ry * 4 + i;
+        const bool here = r < w.rows;
+        float* out = p.splits > 1 ? smem + r * DM : here ? (float*)a.o + w.at(p, a.so, r) : nullptr;
+        const float f = p.splits > 1 ? 1.f : w.len ? 1.f / ll[i] : 0.f;
+#pragma unroll
+        for (int u = 0; u < NC; u += 2) {
+            const int d = u < C::QUADS * 4 ? (u / 4) * 32 + cx * 4 + u % 4 : C::QUADS * 32 + cx * 2;
+            float lo, hi;
+            unpack2(o[i][u / 2], lo, hi);
+            if (p.splits > 1 || (here && d < a.D)) { out[d] = lo * f; out[d + 1] = hi * f; }
         }
     }
     if (p.splits > 1) {
@@ -216,9 +229,9 @@ __global__ void __launch_bounds__(THREADS, 2) xattn_f32_kernel(const RowParams p
     }
 }
 
-template <int NC> cudaError_t launch(const XAttnArgs& a, cudaStream_t s) {
-    const RowParams p = plan_rows<xattn_f32_kernel<NC>>(a, THREADS, ROWS, Cfg<NC>::SMEM, Cfg<NC>::KEYS);
-    return cc::launch_clusters<xattn_f32_kernel<NC>>({(int64_t)p.groups * a.Hkv * a.B * p.splits, THREADS, Cfg<NC>::SMEM, Cfg<NC>::SMEM, p.splits}, s, p);
+template <int DM> cudaError_t launch(const XAttnArgs& a, cudaStream_t s) {
+    const RowParams p = plan_rows<xattn_f32_kernel<DM>>(a, THREADS, ROWS, Cfg<DM>::SMEM, Cfg<DM>::KEYS);
+    return cc::launch_clusters<xattn_f32_kernel<DM>>({(int64_t)p.groups * a.Hkv * a.B * p.splits, THREADS, Cfg<DM>::SMEM, Cfg<DM>::SMEM, p.splits}, s, p);
 }
 
 }  // namespace
@@ -230,13 +243,12 @@ bool xattn_f32_supported(const XAttnArgs& a) {
 }
 
 cudaError_t launch_xattn_f32(const XAttnArgs& a, cudaStream_t s) {
-    const int nc = (a.D + 15) / 16;
-    if (nc <= 2) return launch<2>(a, s);
-    if (nc <= 3) return launch<3>(a, s);
-    if (nc <= 4) return launch<4>(a, s);
-    if (nc <= 5) return launch<5>(a, s);
-    if (nc <= 6) return launch<6>(a, s);
-    return launch<8>(a, s);
+    if (a.D <= 32) return launch<32>(a, s);
+    if (a.D <= 48) return launch<48>(a, s);
+    if (a.D <= 64) return launch<64>(a, s);
+    if (a.D <= 80) return launch<80>(a, s);
+    if (a.D <= 96) return launch<96>(a, s);
+    return launch<128>(a, s);
 }
 
 }  // namespace vd
