@@ -1,12 +1,12 @@
 // Attention to states of another length in single precision, on the FP32 pipes (no operand or sum in fewer bits; the tensor core
-// drops what falls off a running sum, and one of several hundred keys shows it).  A CTA of 128 threads takes 64 rows of a key head
-// (a row: a token and one of the heads that share it) and walks blocks of 16 NJ keys; two CTAs share an SM, so that one computes
-// while the other exchanges.  All products are fma.rn.f32x2 on pairs that lie in shared memory as they are needed: a move that makes a
-// pair of one number runs on the same pipes (they cost a quarter of the time).
-//   scores   8 rows x NJ keys of a thread, pairs along the channels.  Its keys are 16 apart and a key's row is an odd multiple of 16
-//            bytes long: no bank conflicts
-//   output   4 rows x DM / 8 channels of a thread, pairs of channels; P is stored as pairs of equal numbers, its 16-byte pieces exchanged by
-//            key.  A warp's 16 rows are its own in either shape, so P needs no barrier
+// drops what falls off a running sum, and one of several hundred keys shows it).  A CTA of 128 threads takes 16 RT rows of a key head
+// (a row: a token and one of the heads that share it) and walks blocks of 8 KJ keys; two CTAs share an SM, so that one computes
+// while the other exchanges.  What bounds it is the way from shared memory to the registers, 128 bytes a clock for all warps, broadcast or
+// not: an fma.rn.f32x2 of a thread may take two of a thread's bytes.  So a thread holds as much as its registers allow:
+//   scores   RT rows x KJ keys, pairs along the channels, so that both operands are pairs as they lie in memory.  Its keys are 8 apart and
+//            a key's row is an odd multiple of 16 bytes long: no bank conflicts
+//   output   the same RT rows x DM / 8 channels, pairs of channels; P goes through shared memory among the 8 threads of a row, its 16-byte
+//            pieces exchanged by key, without a barrier
 // k, v and q come by cp.async, k and v one step ahead of their use.  Where there are few rows a cluster divides the keys (xattn_meet.cuh).
 #include "block_ops.h"
 #include "xattn_meet.cuh"
@@ -17,13 +17,13 @@ namespace {
 using namespace tc;
 using namespace xa;
 
-constexpr int ROWS = 64, THREADS = 128;
+constexpr int THREADS = 128;
 
 template <int DM_> struct Cfg {                              // DM: channels that are held, a multiple of 16
-    static constexpr int DM = DM_, NJ = DM > 96 ? 3 : 4, KEYS = NJ * 16;
+    static constexpr int DM = DM_, RT = DM > 80 ? 4 : 8, KJ = DM > 80 ? 8 : 6, ROWS = 16 * RT, KEYS = 8 * KJ;
     static constexpr int NC = DM / 8, QUADS = NC / 4, REST = NC % 4;     // channels of a thread's output: QUADS times four, 32 apart, and two more
-    // Q [64][DM], K [KEYS][DM + 4], V [KEYS][DM], P [KEYS][64] pairs
-    static constexpr int Q_AT = 0, K_AT = ROWS * DM, V_AT = K_AT + KEYS * (DM + 4), P_AT = V_AT + KEYS * DM, END = P_AT + KEYS * ROWS * 2;
+    // Q [ROWS][DM], K [KEYS][DM + 4], V [KEYS][DM], P [KEYS][ROWS]
+    static constexpr int Q_AT = 0, K_AT = ROWS * DM, V_AT = K_AT + KEYS * (DM + 4), P_AT = V_AT + KEYS * DM, END = P_AT + KEYS * ROWS;
     static constexpr int SMEM = END * 4;
     static_assert((DM + 4) % 8 == 4 && (REST == 0 || REST == 2), "an odd multiple of 16 bytes; whole pairs");
     static_assert(2 * (SMEM + 1024) <= 228 * 1024, "two CTAs share an SM");
@@ -33,146 +33,147 @@ template <int DM_> struct Cfg {                              // DM: channels tha
 template <int DM>
 __global__ void __launch_bounds__(THREADS, 2) xattn_f32_kernel(const RowParams p) {
     using C = Cfg<DM>;
-    constexpr int NJ = C::NJ, KEYS = C::KEYS, KS = DM + 4, NC = C::NC;
+    constexpr int RT = C::RT, KJ = C::KJ, ROWS = C::ROWS, KEYS = C::KEYS, KS = DM + 4, NC = C::NC;
     extern __shared__ __align__(16) float smem[];
     float *s_q = smem + C::Q_AT, *s_k = smem + C::K_AT, *s_v = smem + C::V_AT, *s_p = smem + C::P_AT;
     const XAttnArgs& a = p.a;
-    const int tid = threadIdx.x, lane = tid & 31, tx = tid & 15, ty = tid >> 4, cx = tid & 7, ry = tid >> 3;     // scores: rows 8 ty, keys tx; output: rows 4 ry
+    const int tid = threadIdx.x, cx = tid & 7, ry = tid >> 3;                // rows RT ry, keys cx, channels 4 cx
     const int split = p.splits > 1 ? (int)cluster_ctarank() : 0;
     const Work w = work_of<ROWS>(p);
     const int tiles = (w.len + KEYS - 1) / KEYS, mine = tiles > split ? (tiles - split + p.splits - 1) / p.splits : 0;
-    const int chunks = a.D / 4, lc = tid & 7, lr = tid >> 3; // loads: eight threads per key or row
-    const float* k = (const float*)a.k + w.b * a.sk.batch + w.kvh * a.sk.head + lc * 4;
-    const float* v = (const float*)a.v + w.b * a.sv.batch + w.kvh * a.sv.head + lc * 4;
+    const int chunks = a.D / 4;                              // loads: eight threads per key or row
+    const float* k = (const float*)a.k + w.b * a.sk.batch + w.kvh * a.sk.head + cx * 4;
+    const float* v = (const float*)a.v + w.b * a.sv.batch + w.kvh * a.sv.head + cx * 4;
     constexpr int CHUNKS = (DM / 4 + 7) / 8;                 // of a thread's part of a key
+    auto chunk_held = [&](int c) { return DM % 32 == 0 || c + 1 < CHUNKS || cx + 8 * c < DM / 4; };
     // zeros where there are no channels or keys (0 * NaN is NaN)
     auto load = [&](float* dst, int stride, const float* src, int64_t token, int key0) {
-        const uint32_t at = smem_u32(dst + lr * stride + lc * 4);
-        const float* row = src + (key0 + lr) * token;
+        const uint32_t at = smem_u32(dst + ry * stride + cx * 4);
+        const float* row = src + (key0 + ry) * token;
 #pragma unroll
         for (int r = 0; r < KEYS; r += 16, row += 16 * token) {
-            const bool here = key0 + r + lr < w.len;
+            const bool here = key0 + r + ry < w.len;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
-                if (DM % 32 == 0 || c + 1 < CHUNKS || lc + 8 * c < DM / 4) {
-                    const bool in = here && lc + 8 * c < chunks;
+                if (chunk_held(c)) {
+                    const bool in = here && cx + 8 * c < chunks;
                     cp_async16(at + (uint32_t)(r * stride + c * 32) * 4u, in ? row + c * 32 : src, in ? 16u : 0u);
                 }
         }
     };
-    for (int r = lr; r < ROWS; r += 16) {
+    for (int r = ry; r < ROWS; r += 16) {
         const bool here = r < w.rows;
-        const float* row = (const float*)a.q + w.at(p, a.sq, here ? r : 0);
-        for (int c = lc; c < DM / 4; c += 8) {
-            const bool in = here && c < chunks;
-            cp_async16(smem_u32(s_q + r * DM + c * 4), in ? row + c * 4 : (const float*)a.q, in ? 16u : 0u);
-        }
+        const float* row = (const float*)a.q + w.at(p, a.sq, here ? r : 0) + cx * 4;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+            if (chunk_held(c)) {
+                const bool in = here && cx + 8 * c < chunks;
+                cp_async16(smem_u32(s_q + r * DM + cx * 4 + c * 32), in ? row + c * 32 : (const float*)a.q, in ? 16u : 0u);
+            }
     }
     if (mine) load(s_k, KS, k, a.sk.token, split * KEYS);
     cp_async_commit();
     if (mine) load(s_v, DM, v, a.sv.token, split * KEYS);
     cp_async_commit();
 
-    unsigned long long o[4][NC / 2];                         // rows 4 ry + i
-    float m_ref[8], l[8];
+    unsigned long long o[RT][NC / 2];
+    float m_ref[RT], l[RT];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < RT; ++i) {
+        m_ref[i] = -INFINITY;
+        l[i] = 0.f;
 #pragma unroll
         for (int u = 0; u < NC / 2; ++u) o[i][u] = 0ull;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { m_ref[i] = -INFINITY; l[i] = 0.f; }
-
+    }
     for (int t = 0; t < mine; ++t) {
         const int key0 = (split + t * p.splits) * KEYS, next = key0 + p.splits * KEYS;
         asm volatile("cp.async.wait_group 1;" ::: "memory"); // K (and Q) of this block
         __syncthreads();
-        float s[8][NJ];
+        float s[RT][KJ];
         {
-            unsigned long long acc[8][NJ];
+            unsigned long long acc[RT][KJ];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < RT; ++i)
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[i][j] = 0ull;
-            const float* qp = s_q + ty * 8 * DM;
-            const float* kp = s_k + tx * KS;
+                for (int j = 0; j < KJ; ++j) acc[i][j] = 0ull;
+            const float* qp = s_q + ry * RT * DM;
+            const float* kp = s_k + cx * KS;
 #pragma unroll 2
             for (int d = 0; d < a.D; d += 4) {
-                ulonglong2 kk[NJ];
+                ulonglong2 kk[KJ];
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) kk[j] = *(const ulonglong2*)(kp + j * 16 * KS + d);
+                for (int j = 0; j < KJ; ++j) kk[j] = *(const ulonglong2*)(kp + j * 8 * KS + d);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < RT; ++i) {
                     const ulonglong2 q = *(const ulonglong2*)(qp + i * DM + d);
 #pragma unroll
-                    for (int j = 0; j < NJ; ++j) acc[i][j] = fmaf2(q.y, kk[j].y, fmaf2(q.x, kk[j].x, acc[i][j]));
+                    for (int j = 0; j < KJ; ++j) acc[i][j] = fmaf2(q.y, kk[j].y, fmaf2(q.x, kk[j].x, acc[i][j]));
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < RT; ++i)
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) s[i][j] = sum2(acc[i][j]) * p.scale_log2;
+                for (int j = 0; j < KJ; ++j) s[i][j] = sum2(acc[i][j]) * p.scale_log2;
         }
         __syncthreads();                                     // K has been read
         if (t + 1 < mine) load(s_k, KS, k, a.sk.token, next);
         cp_async_commit();
         if (key0 + KEYS > w.len)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
-                if (key0 + tx + 16 * j >= w.len)
+            for (int j = 0; j < KJ; ++j)
+                if (key0 + cx + 8 * j >= w.len)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) s[i][j] = -INFINITY;
+                    for (int i = 0; i < RT; ++i) s[i][j] = -INFINITY;
         bool grow = false;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < RT; ++i) {
             float top = s[i][0];
 #pragma unroll
-            for (int j = 1; j < NJ; ++j) top = fmaxf(top, s[i][j]);
+            for (int j = 1; j < KJ; ++j) top = fmaxf(top, s[i][j]);
             grow = grow || top > m_ref[i] + RESCALE_THRESHOLD;
         }
-        if (__any_sync(0xffffffffu, grow)) {                 // (a row's 16 threads sit in one half of a warp)
-            float f[8];
+        if (__any_sync(0xffffffffu, grow)) {                 // (a row's 8 threads sit side by side)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < RT; ++i) {
                 float top = m_ref[i];
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) top = fmaxf(top, s[i][j]);
+                for (int j = 0; j < KJ; ++j) top = fmaxf(top, s[i][j]);
 #pragma unroll
-                for (int x = 1; x < 16; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-                f[i] = top == -INFINITY ? 1.f : ex2(m_ref[i] - top);
+                for (int x = 1; x < 8; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                const float f = top == -INFINITY ? 1.f : ex2(m_ref[i] - top);
                 m_ref[i] = top;
-                l[i] *= f[i];
-            }
+                l[i] *= f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {                    // row 4 ry + i: the factor is with lane 16 (ry & 2) / 2, number 4 (ry & 1) + i
-                const float lo = __shfl_sync(0xffffffffu, f[i], (lane >> 4) << 4), hi = __shfl_sync(0xffffffffu, f[i + 4], (lane >> 4) << 4);
-                const float g = ry & 1 ? hi : lo;
-#pragma unroll
-                for (int u = 0; u < NC / 2; ++u) o[i][u] = fmaf2(o[i][u], pack2(g, g), 0ull);
+                for (int u = 0; u < NC / 2; ++u) o[i][u] = fmaf2(o[i][u], pack2(f, f), 0ull);
             }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < RT; ++i) {
             const float ref = m_ref[i] == -INFINITY ? 0.f : m_ref[i];
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
+            for (int j = 0; j < KJ; ++j) {
                 s[i][j] = ex2(s[i][j] - ref);
                 l[i] += s[i][j];
             }
         }
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {                       // pieces of two rows, exchanged by key
-            float* row = s_p + (tx + 16 * j) * (ROWS * 2);
+        for (int j = 0; j < KJ; ++j) {                       // pieces of four rows, exchanged by key
+            float* row = s_p + (cx + 8 * j) * ROWS;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *(float4*)(row + (((ty * 4 + i) ^ (tx & 7)) << 2)) = make_float4(s[2 * i][j], s[2 * i][j], s[2 * i + 1][j], s[2 * i + 1][j]);
+            for (int h = 0; h < RT / 4; ++h)
+                *(float4*)(row + (((ry * (RT / 4) + h) ^ cx) << 2)) = make_float4(s[4 * h][j], s[4 * h + 1][j], s[4 * h + 2][j], s[4 * h + 3][j]);
         }
         asm volatile("cp.async.wait_group 1;" ::: "memory"); // V of this block
         __syncthreads();
 #pragma unroll 8
         for (int key = 0; key < KEYS; ++key) {
-            // (this warp's two pieces lie side by side, the other way round where the key is odd)
-            const float* row = s_p + key * (ROWS * 2) + (((ry * 2) ^ (key & 6)) << 2);
-            const ulonglong2 pa = *(const ulonglong2*)row, pb = *(const ulonglong2*)(row + 4), p0 = key & 1 ? pb : pa, p1 = key & 1 ? pa : pb;
+            const float* row = s_p + key * ROWS;
+            float pr[RT];
+#pragma unroll
+            for (int h = 0; h < RT / 4; ++h) {
+                const float4 x = *(const float4*)(row + (((ry * (RT / 4) + h) ^ (key & 7)) << 2));
+                pr[4 * h] = x.x; pr[4 * h + 1] = x.y; pr[4 * h + 2] = x.z; pr[4 * h + 3] = x.w;
+            }
             unsigned long long vv[NC / 2];
             const float* at = s_v + key * DM;
 #pragma unroll
@@ -182,39 +183,28 @@ __global__ void __launch_bounds__(THREADS, 2) xattn_f32_kernel(const RowParams p
             }
             if (C::REST) vv[NC / 2 - 1] = *(const unsigned long long*)(at + C::QUADS * 32 + cx * 2);
 #pragma unroll
-            for (int u = 0; u < NC / 2; ++u) {
-                o[0][u] = fmaf2(p0.x, vv[u], o[0][u]);
-                o[1][u] = fmaf2(p0.y, vv[u], o[1][u]);
-                o[2][u] = fmaf2(p1.x, vv[u], o[2][u]);
-                o[3][u] = fmaf2(p1.y, vv[u], o[3][u]);
+            for (int i = 0; i < RT; ++i) {
+                const unsigned long long x = pack2(pr[i], pr[i]);
+#pragma unroll
+                for (int u = 0; u < NC / 2; ++u) o[i][u] = fmaf2(x, vv[u], o[i][u]);
             }
         }
-        __syncthreads();                                     // V has been read (and P, by its warp)
+        __syncthreads();                                     // V has been read (and P, by its threads)
         if (t + 1 < mine) load(s_v, DM, v, a.sv.token, next);
         cp_async_commit();
     }
     cp_async_wait_all();
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int x = 1; x < 16; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
     float2* om = (float2*)(smem + ROWS * DM);
     if (p.splits > 1) __syncthreads();                       // the meeting's memory lies over the stages
-    float ll[4];                                             // of rows 4 ry + i, like the factors above
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float lo = __shfl_sync(0xffffffffu, l[i], (lane >> 4) << 4), hi = __shfl_sync(0xffffffffu, l[i + 4], (lane >> 4) << 4);
-        ll[i] = ry & 1 ? hi : lo;
-    }
-    if (p.splits > 1 && tx == 0)
+    for (int i = 0; i < RT; ++i) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) om[ty * 8 + i] = make_float2(m_ref[i], l[i]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = ry * 4 + i;
+        for (int x = 1; x < 8; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+        const int r = ry * RT + i;
         const bool here = r < w.rows;
+        if (p.splits > 1 && cx == 0) om[r] = make_float2(m_ref[i], l[i]);
         float* out = p.splits > 1 ? smem + r * DM : here ? (float*)a.o + w.at(p, a.so, r) : nullptr;
-        const float f = p.splits > 1 ? 1.f : w.len ? 1.f / ll[i] : 0.f;
+        const float f = p.splits > 1 ? 1.f : w.len ? 1.f / l[i] : 0.f;
 #pragma unroll
         for (int u = 0; u < NC; u += 2) {
             const int d = u < C::QUADS * 4 ? (u / 4) * 32 + cx * 4 + u % 4 : C::QUADS * 32 + cx * 2;
@@ -230,7 +220,7 @@ __global__ void __launch_bounds__(THREADS, 2) xattn_f32_kernel(const RowParams p
 }
 
 template <int DM> cudaError_t launch(const XAttnArgs& a, cudaStream_t s) {
-    const RowParams p = plan_rows<xattn_f32_kernel<DM>>(a, THREADS, ROWS, Cfg<DM>::SMEM, Cfg<DM>::KEYS);
+    const RowParams p = plan_rows<xattn_f32_kernel<DM>>(a, THREADS, Cfg<DM>::ROWS, Cfg<DM>::SMEM, Cfg<DM>::KEYS);
     return cc::launch_clusters<xattn_f32_kernel<DM>>({(int64_t)p.groups * a.Hkv * a.B * p.splits, THREADS, Cfg<DM>::SMEM, Cfg<DM>::SMEM, p.splits}, s, p);
 }
 
