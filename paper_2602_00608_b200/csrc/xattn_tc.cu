@@ -31,7 +31,7 @@ constexpr int HALF = KEYS / 2;                               // keys of P that g
 constexpr int SOFTMAX_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, NUM_THREADS = 352;     // MMA_WARP + s issues for tile s
 constexpr int MAX_LENS = 128;                                // lengths that are kept in shared memory
 constexpr int MAX_SPLITS = xa::MAX_SPLITS;
-constexpr double MEET_TILES = 8.0;                           // what a meeting costs, in tiles
+constexpr double MEET_REST = 8.0, MEET_ALL = 5.0;            // what a meeting costs, in tiles
 constexpr float RESCALE_THRESHOLD = 8.0f;                    // log2 units: accumulators may grow by 2^8
 
 template <int DP> struct Cfg {
@@ -373,9 +373,11 @@ __device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
 }
 // The CTAs of a cluster have each taken a share of an item's keys: they show one another half of the channels at a time, in fp32, and each
 // adds up (in the order of the shares) and writes its part of the tile's rows.  By the 128 threads of tile s; `rounds` counts what these
-// have shown so far.  Out of line: few items come here, and the softmax has no registers to spare.
-template <int DP>
-__device__ __noinline__ void meet(const Params& a, const Items<true>& it, Bars* bars, uint8_t* show, float2* ml, float2 mine, uint32_t t_o, int s, int row, uint32_t rounds) {
+// have shown so far.  A load of another CTA's memory takes 900 cycles.  FAST: a thread has a row, its weights in registers and all shares'
+// loads under way at once (18000 instead of 29000 cycles a meeting, 2 x 300 x 3000, 8 heads of 128, 36 -> 29 us), which crowds the softmax's
+// registers: calls with whole items besides take the loops, out of line (5400 x 14400, 16 heads of 128 519 us, FAST 546).
+template <int DP, bool FAST>
+__device__ __forceinline__ void meet_inline(const Params& a, const Items<true>& it, Bars* bars, uint8_t* show, float2* ml, float2 mine, uint32_t t_o, int s, int row, uint32_t rounds) {
     constexpr int COLS = DP / 2, PIECES = COLS / 4;          // of a round; 16-byte pieces of them
     volatile uint32_t* abort_flag = &bars->abort_flag;
     const int rank = (int)cluster_ctarank();
@@ -387,6 +389,12 @@ __device__ __noinline__ void meet(const Params& a, const Items<true>& it, Bars* 
         (void)cc::wait_cluster(smem_u32(bar), parity, abort_flag);
         __syncwarp();
     };
+    const int r0 = ROWS * rank / a.splits, r1 = ROWS * (rank + 1) / a.splits;
+    // FAST: this thread's row of the CTA's part, and how many threads it has
+    const int per_row = ROWS / ((ROWS + a.splits - 1) / a.splits), r = r0 + row / per_row, tt = r / a.g, t = it.t0 + s * a.nt + tt;
+    const bool mine_to_write = r < r1 && tt < a.nt && t < a.Tq;
+    __nv_bfloat16* out = a.o + it.b * a.o_batch + t * a.o_token + (it.kvh * a.g + r - tt * a.g) * a.o_head;
+    float f[MAX_SPLITS];                                     // the shares' weights
     for (int round = 0; round < 2; ++round, ++rounds) {
         if (rounds > 0) hear(&bars->seen[s], (rounds - 1) & 1);      // everybody has read what was shown last
         if (round == 0) ml[row] = mine;
@@ -406,12 +414,47 @@ __device__ __noinline__ void meet(const Params& a, const Items<true>& it, Bars* 
         }
         tell(&bars->shown[s]);
         hear(&bars->shown[s], rounds & 1);
-        const int r0 = ROWS * rank / a.splits, r1 = ROWS * (rank + 1) / a.splits;
-        for (int i = r0 * PIECES + row; i < r1 * PIECES; i += ROWS) {
+        if (FAST && mine_to_write) {
+            if (round == 0) {
+                const uint32_t at = smem_u32(ml + r);
+                float2 w[MAX_SPLITS];
+#pragma unroll
+                for (int k = 0; k < MAX_SPLITS; ++k)
+                    if (k < a.splits) w[k] = ld_cluster2(map_to_cta(at, (uint32_t)k));
+                float top = -INFINITY, l = 0.f;
+#pragma unroll
+                for (int k = 0; k < MAX_SPLITS; ++k)
+                    if (k < a.splits) top = fmaxf(top, w[k].x);
+                const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+                for (int k = 0; k < MAX_SPLITS; ++k)
+                    if (k < a.splits) { f[k] = ex2(w[k].x - ref); l = fmaf(f[k], w[k].y, l); }
+#pragma unroll
+                for (int k = 0; k < MAX_SPLITS; ++k)
+                    if (k < a.splits) f[k] /= l;
+            }
+            for (int piece = row % per_row; piece < PIECES; piece += per_row) {
+                const int d = round * COLS + piece * 4;
+                if (d >= a.D) break;
+                const uint32_t at = smem_u32(show + r * (COLS * 4) + ((piece ^ (r & (PIECES - 1))) << 4));
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int k0 = 0; k0 < MAX_SPLITS; k0 += 4) {
+                    float4 v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k0 + k < a.splits) v[k] = ld_cluster4(map_to_cta(at, (uint32_t)(k0 + k)));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k0 + k < a.splits) { const float g = f[k0 + k]; o.x = fmaf(g, v[k].x, o.x); o.y = fmaf(g, v[k].y, o.y); o.z = fmaf(g, v[k].z, o.z); o.w = fmaf(g, v[k].w, o.w); }
+                }
+                *(uint2*)(out + d) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
+            }
+        }
+        for (int i = FAST ? r1 * PIECES : r0 * PIECES + row; i < r1 * PIECES; i += ROWS) {
             const int r = i / PIECES, piece = i % PIECES, tt = r / a.g, t = it.t0 + s * a.nt + tt, d = round * COLS + piece * 4;
             if (tt >= a.nt || t >= a.Tq || d >= a.D) continue;
             const uint32_t at = smem_u32(show + r * (COLS * 4) + ((piece ^ (r & (PIECES - 1))) << 4)), at_ml = smem_u32(ml + r);
-            // (loads of other CTAs' memory take a thousand cycles: some at a time, but not so many that the call's registers crowd the softmax's)
             float top = -INFINITY;
 #pragma unroll 4
             for (int k = 0; k < a.splits; ++k) top = fmaxf(top, ld_cluster2(map_to_cta(at_ml, (uint32_t)k)).x);
@@ -430,17 +473,24 @@ __device__ __noinline__ void meet(const Params& a, const Items<true>& it, Bars* 
             *(uint2*)(a.o + it.b * a.o_batch + t * a.o_token + (it.kvh * a.g + r - tt * a.g) * a.o_head + d) =
                 make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
         }
+        __syncwarp();
         tell(&bars->seen[s]);
     }
 }
+template <int DP>
+__device__ __noinline__ void meet_out_of_line(const Params& a, const Items<true>& it, Bars* bars, uint8_t* show, float2* ml, float2 mine, uint32_t t_o, int s, int row, uint32_t rounds) {
+    meet_inline<DP, false>(a, it, bars, show, ml, mine, t_o, s, row, rounds);
+}
 
-// SPLIT: some items are divided by keys among the CTAs of a cluster (a build of its own: the code costs the short items 20 % even where it is
-// not reached)
-template <int DP, bool SPLIT>
+// DIVIDED: by keys among the CTAs of a cluster are no items, those that whole rounds leave over, or all (builds of their own: the code costs
+// short items 20 % even where it is not reached)
+enum { NONE = 0, REST = 1, ALL = 2 };
+template <int DP, int DIVIDED>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                 const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o) {
     using C = Cfg<DP>;
+    constexpr bool SPLIT = DIVIDED != NONE;
     extern __shared__ __align__(1024) uint8_t smem_q[];
     if (smem_u32(smem_q) & 1023u) return;                    // (it is: the swizzle needs it)
     uint8_t* smem_o = smem_q + C::Q_BUFS * 2 * C::TILE_BYTES;
@@ -509,7 +559,9 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
                 if (it.split && it.tiles) {
                     if (out_thread) bulk_wait_group_read<0>();
                     named_barrier_sync(1 + s, ROWS);
-                    meet<DP>(a, it, bars, smem_o + s * C::TILE_BYTES, ml + s * ROWS, make_float2(m_ref, it.n ? l : 0.f), t_o, s, row, n_meet);
+                    const float2 mine = make_float2(m_ref, it.n ? l : 0.f);
+                    if constexpr (DIVIDED == ALL) meet_inline<DP, true>(a, it, bars, smem_o + s * C::TILE_BYTES, ml + s * ROWS, mine, t_o, s, row, n_meet);
+                    else meet_out_of_line<DP>(a, it, bars, smem_o + s * C::TILE_BYTES, ml + s * ROWS, mine, t_o, s, row, n_meet);
                     n_meet += 2;
                     tc_fence_before();
                     continue;
@@ -774,11 +826,12 @@ template <int DP> Division divide(uint32_t items, int Tk, int sms) {
     Division best{1, items, std::min(items, (uint32_t)sms)};
     double cost = (double)((items + best.grid - 1) / best.grid) * (double)(tiles + 1);
     for (int n = 2; n <= MAX_SPLITS && n <= tiles; ++n) {
-        const int held = xa::clusters_held<xattn_tc_kernel<DP, true>>(NUM_THREADS, Cfg<DP>::SMEM, n);
+        const int held = xa::clusters_held<xattn_tc_kernel<DP, ALL>>(NUM_THREADS, Cfg<DP>::SMEM, n);      // (REST has the same shape)
         if (held < 1) continue;
         const uint32_t ctas = (uint32_t)(held * n), whole = items / ctas * ctas, left = items - whole;
         if (left == 0) continue;
-        const double c = (double)(whole / ctas) * (double)(tiles + 1) + (double)((left + held - 1) / held) * ((double)((tiles + n - 1) / n) + MEET_TILES);
+        const double c = (double)(whole / ctas) * (double)(tiles + 1) +
+                         (double)((left + held - 1) / held) * ((double)((tiles + n - 1) / n) + (whole ? MEET_REST : MEET_ALL));
         if (c < cost) { cost = c; best = {n, whole, whole ? ctas : std::min(left, (uint32_t)held) * (uint32_t)n}; }
     }
     return best;
@@ -793,8 +846,9 @@ template <int DP> cudaError_t launch(Params& p, const CUtensorMap& tq, const CUt
     p.dq = (int)(grid % (uint32_t)p.q_items);
     p.dh = (int)(heads % (uint32_t)p.Hkv);
     p.db = (int)(heads / (uint32_t)p.Hkv);
-    if (p.splits > 1) return cc::launch_clusters<xattn_tc_kernel<DP, true>>({grid, NUM_THREADS, smem, smem, p.splits}, s, p, tq, tk, tv, to);
-    return cc::launch_clusters<xattn_tc_kernel<DP, false>>({grid, NUM_THREADS, smem, smem, 1}, s, p, tq, tk, tv, to);
+    if (p.splits > 1 && p.whole) return cc::launch_clusters<xattn_tc_kernel<DP, REST>>({grid, NUM_THREADS, smem, smem, p.splits}, s, p, tq, tk, tv, to);
+    if (p.splits > 1) return cc::launch_clusters<xattn_tc_kernel<DP, ALL>>({grid, NUM_THREADS, smem, smem, p.splits}, s, p, tq, tk, tv, to);
+    return cc::launch_clusters<xattn_tc_kernel<DP, NONE>>({grid, NUM_THREADS, smem, smem, 1}, s, p, tq, tk, tv, to);
 }
 
 }  // namespace
