@@ -36,7 +36,7 @@ typedef enum {
 typedef struct {
     uint32_t struct_size;
     int32_t dtype;              /* vd_dtype of q, k, v and o */
-    int32_t batch, q_len, kv_len;       /* >= 0; batch * heads * q_len and kv_len at most 2^30 */
+    int32_t batch, q_len, kv_len;       /* >= 0; batch * heads * q_len at most 2^30, kv_len at most 2^25 */
     int32_t heads, kv_heads;    /* heads a multiple of kv_heads */
     int32_t head_dim;           /* 1..256 */
     int32_t impl;               /* vd_xattn_impl */

@@ -535,6 +535,11 @@ def _block_dtype(t, name: str) -> int:
     return VD_F32
 
 
+def _sizes_fit(*tensors):
+    if any(n >= 1 << 31 for t in tensors for n in t.shape):
+        _refuse("a size of 2^31 or more")
+
+
 def _on_device(ref, **others):
     if not ref.is_cuda:
         _refuse("tensors must be on a CUDA device")
@@ -575,6 +580,7 @@ def _describe_cross_attention(q, k, v, kv_lens, scale, out, impl):
         _refuse("out must have q's shape")
     if not q.dtype == k.dtype == v.dtype == out.dtype:
         _refuse("q, k, v and out must have one type")
+    _sizes_fit(q, k)
     _on_device(q, k=k, v=v, kv_lens=kv_lens, out=out)
     if kv_lens is not None and (kv_lens.dtype != torch.int32 or kv_lens.shape != (b,) or not kv_lens.is_contiguous()):
         _refuse("kv_lens must be a contiguous int32 tensor [B]")
@@ -627,6 +633,9 @@ def _describe_rotary(x, freqs, positions, layout, axis_pairs, amplitude, first_p
         _refuse("layout: half or interleaved")
     if out.shape != x.shape or out.dtype != x.dtype:
         _refuse("out must have x's shape and type")
+    _sizes_fit(x)
+    if abs(first_position) > 1 << 40:
+        _refuse("first_position beyond 2^40")
     _on_device(x, freqs=freqs, positions=positions, out=out)
     pb = pt = 0
     if positions is not None:
@@ -667,8 +676,9 @@ def _describe_gate_norm(x, h, gate, scale, shift, kind, eps, weight, bias, post_
     if kind not in ("layer", "rms"):
         _refuse("kind: layer or rms")
     mod_tokens = max(t, 1) if mod_tokens is None else mod_tokens
-    if mod_tokens < 1:
-        _refuse("mod_tokens must be positive")
+    if not 1 <= mod_tokens < 1 << 31:
+        _refuse("mod_tokens must be positive, below 2^31")
+    _sizes_fit(x)
     for name, o in (("x_out", x_out), ("y", y)):
         if o is not None and o.shape != x.shape:
             _refuse(f"{name} must have x's shape")

@@ -52,7 +52,7 @@ vd_status vd_op_cross_attention(const vd_xattn_desc* d, const void* q, const voi
     if (d->struct_size != sizeof(vd_xattn_desc)) return refuse(VD_ERR_INVALID_ARG, "vd_xattn_desc: struct_size mismatch");
     if (!is_dtype(d->dtype)) return refuse(VD_ERR_INVALID_ARG, "bad dtype");
     if (d->batch < 0 || d->q_len < 0 || d->kv_len < 0 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0 ||
-        d->head_dim < 1 || d->head_dim > 256 || d->kv_len > 1 << 30 || !fits(d->batch, d->heads, d->q_len) ||
+        d->head_dim < 1 || d->head_dim > 256 || d->kv_len > 1 << 25 || !fits(d->batch, d->heads, d->q_len) ||
         (int64_t)d->batch * d->heads * d->q_len > 1 << 30)
         return refuse(VD_ERR_INVALID_ARG, "bad attention sizes");
     if (d->impl < VD_XATTN_AUTO || d->impl > VD_XATTN_PLAIN) return refuse(VD_ERR_INVALID_ARG, "bad impl");

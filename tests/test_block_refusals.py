@@ -36,7 +36,7 @@ def test_struct_sizes_match_the_header_layout():
     dict(head_dim=0), dict(head_dim=257), dict(impl=9), dict(impl=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf), dict(scale=math.nan),
     dict(q_token=-1), dict(o_batch=-5), dict(o_token=0), dict(o_head=63), dict(o_batch=0), dict(o_batch=767),
     dict(batch=1 << 20, q_len=1 << 20), dict(batch=1 << 15, heads=1 << 14, kv_heads=1, q_len=4),
-    dict(kv_len=(1 << 30) + 1), dict(batch=1, heads=2, kv_heads=2, q_len=(1 << 29) + 1),
+    dict(kv_len=(1 << 25) + 1), dict(batch=1, heads=2, kv_heads=2, q_len=(1 << 29) + 1),
 ])
 def test_cross_attention_refuses(change):
     assert vd.lib().vd_op_cross_attention(ctypes.byref(xattn(**change)), P, P, P, None, P, None) == vd.VD_ERR_INVALID_ARG
@@ -172,3 +172,18 @@ def test_the_wrappers_refuse_tensors_that_are_not_on_a_device():
         with pytest.raises(vd.VdError) as e:
             call()
         assert e.value.status == vd.VD_ERR_INVALID_ARG and "device" in str(e.value)
+
+
+def test_the_wrappers_refuse_sizes_that_would_wrap():
+    """2^31 + 5 tokens of stride 0 as an int32 would be a negative number, 2^32 + 5 would be five."""
+    import torch
+    big = torch.zeros(1).expand(1, 2 ** 32 + 5, 1, 8)
+    ok = torch.zeros(1, 2, 1, 8)
+    for call in (lambda: vd._describe_cross_attention(ok, big, big, None, None, ok, 0), lambda: vd._describe_cross_attention(big, ok, ok, None, None, big, 0),
+                 lambda: vd._describe_rotary(big, torch.zeros(4, dtype=torch.float64), None, "half", None, 1.0, 0, big),
+                 lambda: vd._describe_rotary(ok, torch.zeros(4, dtype=torch.float64), None, "half", None, 1.0, 1 << 63, ok),
+                 lambda: vd._describe_gate_norm(big[:, :, 0], None, None, None, None, "rms", 1e-6, None, None, False, None, 1.0, None, big[:, :, 0], None),
+                 lambda: vd._describe_gate_norm(ok[:, :, 0], None, None, None, None, "rms", 1e-6, None, None, False, None, 1.0, 1 << 32, ok[:, :, 0], None)):
+        with pytest.raises(vd.VdError) as e:
+            call()
+        assert e.value.status == vd.VD_ERR_INVALID_ARG and "device" not in str(e.value)

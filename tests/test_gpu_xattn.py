@@ -214,3 +214,46 @@ def test_offsets_beyond_32_bits(vd, tq):
     for f, x in zip(far, (k, v)):
         f.copy_(x)
     run(vd, q, *far)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tq", [1, 2, 40])
+def test_many_sequences(vd, dtype, tq):
+    """More batch items than a CTA keeps lengths of, every length from none to all."""
+    b, tk = 300, 150
+    run(vd, *make(dtype, b, tq, tk, 2, 1, 64, seed=11), lens=[i % (tk + 1) for i in range(b)])
+
+
+def test_a_first_call_can_be_captured():
+    """In a process of its own: nothing of the library has run before the capture."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2602_00608_b200 import binding as vd
+q, k, v = (torch.randn(1, n, 4, 64, device="cuda").bfloat16() for n in (200, 900, 900))
+x = torch.randn(1, 200, 256, device="cuda")
+freqs = vd.rotary_frequencies(64).cuda()
+outs = [torch.empty_like(q), torch.empty_like(q), torch.empty_like(q[:, :1]), torch.empty_like(x), torch.empty_like(x), torch.empty_like(q.float())]
+def step():
+    vd.op_rotary(q, freqs, out=outs[0])
+    vd.op_cross_attention(outs[0], k, v, out=outs[1])
+    vd.op_cross_attention(outs[0][:, :1], k, v, out=outs[2])
+    vd.op_gate_norm(x, x_out=outs[3], y=outs[4])
+    vd.op_cross_attention(q.float(), k.float(), v.float(), out=outs[5])
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    step()
+g.replay()
+torch.cuda.synchronize()
+first = [o.clone() for o in outs]
+step()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(first, outs))
+print("captured")
+"""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
