@@ -499,9 +499,28 @@ def op_attention(qkv, channels: int, scale: float, impl=VD_IMPL_AUTO):
 
 
 # ---- operators of a latent world model's transformer block (include/vd_block.h) -----------------
-# A call's checks and its descriptor follow from the tensors' types, shapes, strides and devices alone, and are kept by these:
-# a token's operators are over on the device before Python has looked at their arguments once more.
+# A call goes through _vd_torch (csrc/vd_torch.cpp), which reads the tensors without Python in between, where that finds nothing to
+# object to: a token's operators are over on the device before Python has looked at ten tensors.  What it leaves (and everything,
+# where it has not been built) takes the way below it: checks that say what is wrong, and a descriptor that follows from the
+# tensors' types, shapes, strides and devices alone, and is kept by these.
+_native = None
 _descriptors = {}
+
+
+def _calls():
+    """The module _vd_torch, told of the library's entry points; False where it is not there."""
+    global _native
+    if _native is None:
+        import torch  # noqa: F401  (its libraries are what the module is linked to)
+        try:
+            from . import _vd_torch as m
+        except ImportError:
+            m = False
+        if m:
+            l = lib()
+            m.bind(*(ctypes.cast(f, c_void_p).value for f in (l.vd_op_cross_attention, l.vd_op_rotary, l.vd_op_gate_norm)))
+        _native = m
+    return _native
 
 
 def _described(key, describe, *args):
@@ -598,6 +617,12 @@ def op_cross_attention(q, k, v, kv_lens=None, scale=None, out=None, impl=VD_XATT
     import torch
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    native = _calls()
+    status = native.cross_attention(q, k, v, kv_lens, scale, out, impl) if native else None
+    if status is not None:
+        if status != VD_OK:
+            _check(status)
+        return out
     desc = _described(("xattn", scale, impl, _sig(q), _sig(k), _sig(v), _sig(kv_lens), _sig(out)), _describe_cross_attention,
                       q, k, v, kv_lens, scale, out, impl)
     _launch(q, lib().vd_op_cross_attention, byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(kv_lens), out.data_ptr())
@@ -662,6 +687,12 @@ def op_rotary(x, freqs, positions=None, *, layout="half", axis_pairs=None, ampli
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     if axis_pairs is not None:
         axis_pairs = tuple(axis_pairs)
+    native = _calls()
+    status = native.rotary(x, freqs, positions, layout, axis_pairs, amplitude, first_position, out) if native else None
+    if status is not None:
+        if status != VD_OK:
+            _check(status)
+        return out
     desc = _described(("rotary", layout, axis_pairs, amplitude, first_position, _sig(x), _sig(freqs), _sig(positions), _sig(out)), _describe_rotary,
                       x, freqs, positions, layout, axis_pairs, amplitude, first_position, out)
     _launch(x, lib().vd_op_rotary, byref(desc), x.data_ptr(), _ptr(positions), freqs.data_ptr(), out.data_ptr())
@@ -724,6 +755,12 @@ def op_gate_norm(x, h=None, *, gate=None, scale=None, shift=None, kind="layer", 
     import torch
     x_out = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if x_out is None else x_out) if want_x else None
     y = (torch.empty(x.shape, dtype=x.dtype if h is None else h.dtype, device=x.device) if y is None else y) if want_y else None
+    native = _calls()
+    status = native.gate_norm(x, h, gate, scale, shift, kind, eps, weight, bias, post_norm, post_weight, residual_scale, mod_tokens, x_out, y) if native else None
+    if status is not None:
+        if status != VD_OK:
+            _check(status)
+        return x_out, y
     desc = _described(("norm", kind, eps, post_norm, residual_scale, mod_tokens, _sig(x), _sig(h), _sig(gate), _sig(scale), _sig(shift), _sig(weight), _sig(bias),
                        _sig(post_weight), _sig(x_out), _sig(y)), _describe_gate_norm,
                       x, h, gate, scale, shift, kind, eps, weight, bias, post_norm, post_weight, residual_scale, mod_tokens, x_out, y)
