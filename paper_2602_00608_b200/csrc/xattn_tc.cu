@@ -34,14 +34,15 @@ constexpr int MAX_SPLITS = xa::MAX_SPLITS;
 constexpr double MEET_REST = 8.0, MEET_ALL = 5.0;            // what a meeting costs, in tiles
 constexpr float RESCALE_THRESHOLD = 8.0f;                    // log2 units: accumulators may grow by 2^8
 
-template <int DP> struct Cfg {
+template <int DP, bool SHORT = false> struct Cfg {
     static constexpr int CHUNKS = DP / CHUNK;
     static constexpr int TILE_BYTES = ROWS * DP * 2;         // of Q (a tile), K or V
-    static constexpr int STAGES = DP == 128 ? 3 : 6, Q_BUFS = DP == 128 ? 1 : 2;
+    static constexpr int STAGES = SHORT ? 2 : DP == 128 ? 3 : 6, Q_BUFS = SHORT || DP == 128 ? 1 : 2, CTAS = SHORT ? 2 : 1;     // CTAS of an SM
     // Tensor memory has room for a P of its own beside the scores where O takes 64 columns: the next scores then do not wait for the
-    // products of P.  Columns of tile s: S at 128 s, O at 256 + DP s, P at P_COL + P_STEP s.
+    // products of P.  Columns of tile s: S at 128 s, O at O_COL + O_STEP s, P at P_COL + P_STEP s.  SHORT: the second half of S is O's.
     static constexpr bool APART = DP == 64;
-    static constexpr uint32_t P_COL = APART ? 384 : 0, P_STEP = APART ? 64 : 128;
+    static constexpr uint32_t TMEM = SHORT ? 256 : 512, P_COL = APART && !SHORT ? 384 : 0, P_STEP = APART && !SHORT ? 64 : 128;
+    static constexpr uint32_t O_COL = SHORT ? 64 : 256, O_STEP = SHORT ? 128 : DP;
     // every so many pairs of exponentials one on the FMA pipes; 0: none.  (They take five instructions for one, and where the products are
     // short the issue slots are what is short.)
     static constexpr int POLY = APART ? 0 : 16;
@@ -52,7 +53,7 @@ struct Bars {
     uint64_t q_full[2], q_empty[2], full[6], empty[6], s_full[2], s_free[2], p_part[2][2], pv_done[2], o_full[2], drained[2], shown[2], seen[2];
     uint32_t tmem_base, abort_flag;
 };
-static_assert(sizeof(Bars) <= 320 && Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448, "shared memory of one CTA");
+static_assert(sizeof(Bars) <= 320 && Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448 && 2 * (Cfg<64, true>::SMEM + 1024) <= 233472, "shared memory of one CTA");
 
 struct Params {
     const int32_t* lens;
@@ -305,9 +306,38 @@ template <int DP> struct Tile {
         hand_over(first_half, lane);
         return top;
     }
-    static __device__ __forceinline__ void mask(uint32_t (&r)[32], int valid) {
+    // The only tile of a row: its maximum is the reference.  Two passes, 32 scores at a time, since two CTAs share the registers.
+    __device__ __forceinline__ float only(int valid) {
+        uint32_t r[32];
+        float top = -INFINITY;
 #pragma unroll
-        for (int q = 0; q < 32; ++q)
+        for (int c = 0; c < KEYS; c += 32)
+            if (c < valid) {
+                tmem_ld32(t_s + (uint32_t)c, r);
+                tmem_ld_wait();
+                if (valid - c < 32) mask(r, valid - c);
+                top = max_of(r, top);
+            }
+        m_ref = top * scale_log2;
+        const unsigned long long sc = pack2(scale_log2, scale_log2), mr = minus_ref();
+#pragma unroll
+        for (int c = 0; c < KEYS; c += 32)
+            if (c < valid) {
+                tmem_ld32(t_s + (uint32_t)c, r);
+                tmem_ld_wait();
+                if (valid - c > 16) {
+                    if (valid - c < 32) mask(r, valid - c);
+                    exp_chunk<0>(r, t_p + (uint32_t)(c >> 1), sc, mr, sum, sum_b);
+                } else {
+                    mask<16>(r, valid - c);
+                    exp_chunk<0, 16>(r, t_p + (uint32_t)(c >> 1), sc, mr, sum, sum_b);
+                }
+            }
+        return top;
+    }
+    template <int N = 32> static __device__ __forceinline__ void mask(uint32_t (&r)[32], int valid) {
+#pragma unroll
+        for (int q = 0; q < N; ++q)
             if (q >= valid) r[q] = __float_as_uint(-INFINITY);
     }
 };
@@ -483,14 +513,17 @@ __device__ __noinline__ void meet_out_of_line(const Params& a, const Items<true>
 }
 
 // DIVIDED: by keys among the CTAs of a cluster are no items, those that whole rounds leave over, or all (builds of their own: the code costs
-// short items 20 % even where it is not reached)
-enum { NONE = 0, REST = 1, ALL = 2 };
+// short items 20 % even where it is not reached).  SHORT: contexts of one tile with heads of up to 64 channels.  An item is then a chain of
+// loads, scores, softmax, output and store with nothing to overlap, so two CTAs share an SM, each with half of its tensor memory (P and O
+// both lie over the scores, which are read twice, 32 at a time: 80 registers a thread): 2 x 10800 x 77, 30 heads of 64 52 -> 41 us (3.2 -> 4.0
+// TB/s), 8 x 1350 x 32, 16 heads 18.7 -> 15.8.
+enum { NONE = 0, REST = 1, ALL = 2, SHORT = 3 };
 template <int DP, int DIVIDED>
-__global__ void __launch_bounds__(NUM_THREADS, 1)
+__global__ void __launch_bounds__(NUM_THREADS, DIVIDED == SHORT ? 2 : 1)
 xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                 const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o) {
-    using C = Cfg<DP>;
-    constexpr bool SPLIT = DIVIDED != NONE;
+    constexpr bool ONE_TILE = DIVIDED == SHORT, SPLIT = DIVIDED == REST || DIVIDED == ALL;
+    using C = Cfg<DP, ONE_TILE>;
     extern __shared__ __align__(1024) uint8_t smem_q[];
     if (smem_u32(smem_q) & 1023u) return;                    // (it is: the swizzle needs it)
     uint8_t* smem_o = smem_q + C::Q_BUFS * 2 * C::TILE_BYTES;
@@ -514,7 +547,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
         fence_proxy_async_smem();
     }
     if (a.lens && tid < min(a.B, MAX_LENS)) lens[tid] = a.lens[tid];
-    if (warp == MMA_WARP) tmem_alloc(smem_u32(&bars->tmem_base), 512);
+    if (warp == MMA_WARP) tmem_alloc(smem_u32(&bars->tmem_base), C::TMEM);
     tc_fence_before();
     __syncthreads();
     if (SPLIT) cluster_sync_all();                    // every CTA's barriers exist before another one arrives on them
@@ -524,7 +557,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
     if (warp < SOFTMAX_WARPS) {
         // ------------------------------------------------------------ softmax: a thread per row
         const int s = warp >> 2, row = (warp & 3) * 32 + lane;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lanes + (uint32_t)s * 128u, t_o = tmem + lanes + 256u + (uint32_t)(s * DP), t_p = tmem + lanes + C::P_COL + (uint32_t)s * C::P_STEP;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lanes + (uint32_t)s * 128u, t_o = tmem + lanes + C::O_COL + (uint32_t)s * C::O_STEP, t_p = tmem + lanes + C::P_COL + (uint32_t)s * C::P_STEP;
         uint8_t* out = smem_o + s * C::TILE_BYTES + row * 128;
         const bool out_thread = (tid & (ROWS - 1)) == 0;
         uint32_t n_s = 0, n_o = 0, n_pv = 0, n_meet = 0;     // tiles, items, waited-for products and rounds of meetings so far
@@ -541,7 +574,9 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
                 Tile<DP> tile{a.scale_log2, t_s, t_p, t_o, j > 0, C::APART && j + 1 < it.n ? &bars->s_free[s] : nullptr,
                               C::APART && j > 0 ? &bars->pv_done[s] : nullptr, n_pv & 1, abort_flag, lane, m_ref, sum, sum_b};
                 if (C::APART && j > 0) ++n_pv;
-                const float tmax = valid >= KEYS ? tile.full(&bars->p_part[s][0]) : valid <= 96 ? tile.most(valid, &bars->p_part[s][0])
+                float tmax;
+                if constexpr (ONE_TILE) tmax = tile.only(valid);
+                else tmax = valid >= KEYS ? tile.full(&bars->p_part[s][0]) : valid <= 96 ? tile.most(valid, &bars->p_part[s][0])
                                                                                             : tile.part(valid, &bars->p_part[s][0]);
                 m_ref = tile.m_ref; sum = tile.sum; sum_b = tile.sum_b;
                 ok = ok && tile.ok;
@@ -587,6 +622,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
 #pragma unroll
                         for (int q = 0; q < 32; ++q) v[q] = 0u;
                     }
+                    if (ONE_TILE && it.tiles && c + 32 >= a.D) hand_over(&bars->s_free[s], lane);      // O, where the next scores come, has been read
 #pragma unroll
                     for (int q = 0; q < 32; q += 8) {
                         float f[8];
@@ -668,7 +704,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
         };
         auto commit = [&](uint64_t* bar) { umma_commit_on(smem_u32(bar), on); };
         auto step = [&]() { if (++st == C::STAGES) { st = 0; ph ^= 1; } };
-        auto issue_qk = [&](int s, uint32_t stage) {
+        auto issue_qk = [&](int s, uint32_t stage, uint32_t idesc_qk) {
             const uint32_t q_lo = desc_lo(smem_u32(smem_q + ((n_q % C::Q_BUFS) * 2 + s) * C::TILE_BYTES)), k_lo = desc_lo(smem_u32(smem_st + stage * C::TILE_BYTES));
 #pragma unroll
             for (int k = 0; k < DP / 16; ++k) {
@@ -681,7 +717,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
         };
         auto issue_pv = [&](int s, uint32_t stage, int from, int steps, bool first) {
             const uint32_t v_lo = desc_lo(smem_u32(smem_st + stage * C::TILE_BYTES)) | (((KEYS * 128u) >> 4) << 16);
-            const uint32_t d = tmem + 256u + (uint32_t)(s * DP), p = tmem + C::P_COL + (uint32_t)s * C::P_STEP;
+            const uint32_t d = tmem + C::O_COL + (uint32_t)s * C::O_STEP, p = tmem + C::P_COL + (uint32_t)s * C::P_STEP;
 #pragma unroll
             for (int i = 0; i < HALF / 16; ++i) {
                 const int k = from + i;
@@ -720,11 +756,12 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
                 }
                 auto scores = [&](bool last) {               // of the next K stage
                     wait_on(&bars->full[st], ph);
-                    issue_qk(s, st);
+                    issue_qk(s, st, ONE_TILE ? make_idesc_bf16(128, (uint32_t)((it.len + 15) & ~15)) : idesc_qk);
                     commit(&bars->empty[st]);
                     if (last) commit(&bars->q_empty[n_q % C::Q_BUFS]);
                     step();
                 };
+                if (ONE_TILE && n_p > 0) wait_on(&bars->s_free[s], (n_p - 1) & 1);
                 scores(it.n == 1);
                 for (int j = 0; j < it.n; ++j) {
                     const int valid = min(KEYS, it.len - (it.j0 + j) * KEYS), steps = (valid + 15) >> 4;
@@ -738,8 +775,9 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
                     clear_rows(st, valid, steps);            // (both warps write the same zeros)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        wait_on(&bars->p_part[s][h], n_p & 1);
-                        issue_pv(s, st, h * (HALF / 16), steps, j == 0);
+                        if (!ONE_TILE || h == 1) wait_on(&bars->p_part[s][h], n_p & 1);
+                        if (ONE_TILE && h == 1) issue_pv(s, st, 0, steps, j == 0);
+                        if (!ONE_TILE || h == 1) issue_pv(s, st, h * (HALF / 16), steps, j == 0);
                     }
                     ++n_p;
                     commit(&bars->empty[st]);
@@ -756,7 +794,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
                 if (*abort_flag) break;
                 wait_on(&bars->q_full[n_q % C::Q_BUFS], (n_q / C::Q_BUFS) & 1);
                 wait_on(&bars->full[st], ph);
-                for (int s = 0; s < it.streams; ++s) issue_qk(s, st);
+                for (int s = 0; s < it.streams; ++s) issue_qk(s, st, idesc_qk);
                 commit(&bars->empty[st]);
                 if (it.n == 1) commit(&bars->q_empty[n_q % C::Q_BUFS]);
                 step();
@@ -779,7 +817,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
                             commit(&bars->o_full[s]);
                         } else {
                             if (s == 0) wait_on(&bars->full[st], ph);
-                            issue_qk(s, st);
+                            issue_qk(s, st, idesc_qk);
                             if (s + 1 == it.streams) {
                                 commit(&bars->empty[st]);
                                 if (j + 2 == it.n) commit(&bars->q_empty[n_q % C::Q_BUFS]);
@@ -804,7 +842,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
     if (SPLIT) cluster_sync_all();                    // nobody leaves while others read its memory
     if (warp == MMA_WARP) {
         tc_fence_after();
-        tmem_dealloc(tmem, 512);
+        tmem_dealloc(tmem, C::TMEM);
     }
 }
 
@@ -838,14 +876,26 @@ template <int DP> Division divide(uint32_t items, int Tk, int sms) {
 }
 
 template <int DP> cudaError_t launch(Params& p, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& to, int sms, cudaStream_t s) {
+    const auto step = [&](uint32_t grid) {
+        const uint32_t heads = grid / (uint32_t)p.q_items;
+        p.dq = (int)(grid % (uint32_t)p.q_items);
+        p.dh = (int)(heads % (uint32_t)p.Hkv);
+        p.db = (int)(heads / (uint32_t)p.Hkv);
+        return grid;
+    };
+    if constexpr (DP == 64)
+        if (p.Tk <= KEYS) {
+            constexpr int short_smem = Cfg<DP, true>::SMEM;
+            p.splits = 1;
+            p.whole = p.items;
+            const uint32_t grid = step(std::min(p.items, 2u * (uint32_t)sms));
+            return cc::launch_clusters<xattn_tc_kernel<DP, SHORT>>({grid, NUM_THREADS, short_smem, short_smem, 1}, s, p, tq, tk, tv, to);
+        }
     constexpr int smem = Cfg<DP>::SMEM;
     const Division d = divide<DP>(p.items, p.Tk, sms);
     p.splits = d.splits;
     p.whole = d.whole;
-    const uint32_t grid = d.grid, heads = grid / (uint32_t)p.q_items;
-    p.dq = (int)(grid % (uint32_t)p.q_items);
-    p.dh = (int)(heads % (uint32_t)p.Hkv);
-    p.db = (int)(heads / (uint32_t)p.Hkv);
+    const uint32_t grid = step(d.grid);
     if (p.splits > 1 && p.whole) return cc::launch_clusters<xattn_tc_kernel<DP, REST>>({grid, NUM_THREADS, smem, smem, p.splits}, s, p, tq, tk, tv, to);
     if (p.splits > 1) return cc::launch_clusters<xattn_tc_kernel<DP, ALL>>({grid, NUM_THREADS, smem, smem, p.splits}, s, p, tq, tk, tv, to);
     return cc::launch_clusters<xattn_tc_kernel<DP, NONE>>({grid, NUM_THREADS, smem, smem, 1}, s, p, tq, tk, tv, to);

@@ -257,3 +257,25 @@ print("captured")
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("size", [(300, 140, 77, 4, 2, 64), (90, 300, 128, 6, 6, 40), (80, 257, 17, 8, 8, 64), (150, 30, 100, 12, 4, 56), (2, 10800, 77, 4, 4, 64)], ids=lambda s: "x".join(map(str, s)))
+def test_short_contexts_of_many_items(vd, size):
+    """Contexts of one tile of keys where a CTA takes several items: every length from none to all, NaN behind each, large scores in between."""
+    import torch
+    b, _, tk = size[:3]
+    q, k, v = make("bf16", *size, seed=12)
+    q[::3] *= 100
+    lens = torch.tensor([(7 * i + tk) % (tk + 1) if b > 2 else tk - 5 * i for i in range(b)], dtype=torch.int32, device="cuda")
+    behind = torch.arange(tk, device="cuda")[None, :, None, None] >= lens[:, None, None, None]
+    scale = q.shape[3] ** -0.5
+    want = block_ref.attention(q, k.masked_fill(behind, 0), v.masked_fill(behind, 0), lens, scale)
+    k.masked_fill_(behind, math.nan)
+    v.masked_fill_(behind, math.nan)
+    first = vd.op_cross_attention(q, k, v, lens, scale=scale)
+    torch.cuda.synchronize()
+    block_ref.check(first, *want)
+    assert (first[lens == 0] == 0).all()
+    again = vd.op_cross_attention(q, k, v, lens, scale=scale)
+    torch.cuda.synchronize()
+    assert torch.equal(first.view(torch.int16), again.view(torch.int16))
