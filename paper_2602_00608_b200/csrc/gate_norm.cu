@@ -97,24 +97,26 @@ __device__ __forceinline__ void unit(float (&z)[NV][V], int C, int lane, int nor
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int e = 0; e < V; ++e) q = fmaf(z[i][e], z[i][e], q);
-    const float rstd = 1.f / sqrtf(token_sum<TPR>(q, red, turn) / n + eps);
+    const float rstd = rsqrtf(token_sum<TPR>(q, red, turn) / n + eps);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int e = 0; e < V; ++e) z[i][e] *= rstd;
 }
 
-// XT: the residual stream; HT: h, y, gate, scale and shift
+// XT: the residual stream; HT: h, y, gate, scale and shift.  (Nine blocks of 128 threads to an SM where a thread has vectors of 8: 21600 tokens
+// of 1920 as the compiler likes it 90 us, eight blocks; nine 86.7; ten 90.)
 template <typename XT, typename HT, int V, int TPR, int NV>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) gate_norm_kernel(const GateNormArgs a) {
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, V == 8 && TPR == 128 ? 9 : 0) gate_norm_kernel(const GateNormArgs a) {
     constexpr int TOKENS = TPR < 128 ? 128 / TPR : 1;        // of a block; a token of several warps has the block to itself
     static_assert(TPR == 32 || TPR >= 128, "");
     __shared__ float red[2][TPR / 32];
     const vd_gate_norm_desc& d = a.d;
-    const int64_t token = (int64_t)blockIdx.x * TOKENS + (TOKENS > 1 ? threadIdx.x / TPR : 0);
-    if (token >= (int64_t)d.batch * d.tokens) return;        // (whole warps)
+    const uint32_t token = blockIdx.x * TOKENS + (TOKENS > 1 ? threadIdx.x / TPR : 0), all = (uint32_t)d.batch * (uint32_t)d.tokens;    // (below 2^31)
+    if (token >= all) return;                                // (whole warps)
     const int lane = TOKENS > 1 ? threadIdx.x % TPR : threadIdx.x;
-    const int b = (int)(token / d.tokens), t = (int)(token % d.tokens), C = d.channels, group = t / d.mod_tokens;
+    const int b = (int)(token / (uint32_t)d.tokens), t = (int)(token - (uint32_t)b * (uint32_t)d.tokens), C = d.channels,
+              group = (int)((uint32_t)t / (uint32_t)d.mod_tokens);
     const XT* x = (const XT*)a.x + b * d.x_batch + t * d.x_token;
     const HT* h = (const HT*)a.h + b * d.h_batch + t * d.h_token;
     int turn = 0;
@@ -298,7 +300,6 @@ template <typename XT, typename HT> cudaError_t launch_typed(const GateNormArgs&
         if (vecs <= 1024) return launch<XT, HT, 8, 512, 2>(a, s);
         return launch<XT, HT, 8, 512, 4>(a, s);
     }
-    // (loads that find no channel cost too: 3039 tokens of 1111, eight a thread 23.3 us, five 18.9)
     // (920 tokens of 4436, bf16, norms on both sides: one channel at a time 49 us, two 21)
     const uint64_t even = d.x_batch | d.x_token | (a.x_out ? d.xo_batch | d.xo_token : 0) | (a.h ? d.h_batch | d.h_token : 0) |
                           (a.y ? d.y_batch | d.y_token : 0) | (a.gate ? d.gate_batch | d.gate_group : 0) |
@@ -316,14 +317,18 @@ template <typename XT, typename HT> cudaError_t launch_typed(const GateNormArgs&
         if (n <= 4096) return launch<XT, HT, 2, 512, 8>(a, s);
         return launch<XT, HT, 2, 512, MAX_CHANNELS / 1024>(a, s);
     }
+    // One channel at a time: the issue slots bound it (600 instructions for a warp's five channels), so few threads with many channels each, the
+    // barriers, divisions and addresses being each warp's; but slots that find no channel cost too.  3039 tokens of 1111, fp32, norms on both
+    // sides: 256 threads of eight 23.3 us, of five 18.6, 128 of nine 16.9; of 2401: 512 of five 51, 256 of ten 39; of 3501: 512 of seven 60, 256 of 14 62.
     if (C <= 128) return launch<XT, HT, 1, 32, 4>(a, s);
     if (C <= 512) return launch<XT, HT, 1, 128, 4>(a, s);
     if (C <= 768) return launch<XT, HT, 1, 128, 6>(a, s);
     if (C <= 1024) return launch<XT, HT, 1, 128, 8>(a, s);
-    if (C <= 1280) return launch<XT, HT, 1, 256, 5>(a, s);
-    if (C <= 1536) return launch<XT, HT, 1, 256, 6>(a, s);
+    if (C <= 1152) return launch<XT, HT, 1, 128, 9>(a, s);
+    if (C <= 1280) return launch<XT, HT, 1, 128, 10>(a, s);
+    if (C <= 1536) return launch<XT, HT, 1, 128, 12>(a, s);
     if (C <= 2048) return launch<XT, HT, 1, 256, 8>(a, s);
-    if (C <= 2560) return launch<XT, HT, 1, 512, 5>(a, s);
+    if (C <= 2560) return launch<XT, HT, 1, 256, 10>(a, s);
     if (C <= 3584) return launch<XT, HT, 1, 512, 7>(a, s);
     if (C <= 5120) return launch<XT, HT, 1, 512, 10>(a, s);
     if (C <= 8192) return launch<XT, HT, 1, 512, 16>(a, s);
