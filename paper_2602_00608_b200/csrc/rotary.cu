@@ -48,9 +48,9 @@ __global__ void __launch_bounds__(MAX_THREADS) rotary_vec_kernel(const RotaryArg
     constexpr int V = 16 / sizeof(T);
     extern __shared__ float2 table[];                        // [tokens][pairs]
     const int pairs = a.R / 2, turning = HALF ? pairs / V : a.R / V, unit = threadIdx.x;
-    const int64_t token = (int64_t)blockIdx.x * blockDim.z + threadIdx.z, tokens = (int64_t)a.B * a.T;
+    const uint32_t token = blockIdx.x * blockDim.z + threadIdx.z, tokens = (uint32_t)a.B * (uint32_t)a.T;      // (below 2^31)
     const bool here = token < tokens, turns = unit < turning;
-    const int b = here ? (int)(token / a.T) : 0, t = here ? (int)(token % a.T) : 0;
+    const int b = here ? (int)(token / (uint32_t)a.T) : 0, t = here ? (int)(token % (uint32_t)a.T) : 0;
     const int c = turns ? unit * V : a.R + (unit - turning) * V;
     const T* x = (const T*)a.x + b * a.sx.batch + t * a.sx.token + c;
     T* y = (T*)a.y + b * a.sy.batch + t * a.sy.token + c;
@@ -69,8 +69,8 @@ __global__ void __launch_bounds__(MAX_THREADS) rotary_vec_kernel(const RotaryArg
             const int n = (int)(blockDim.x * blockDim.y * blockDim.z);
             for (int i = ((int)threadIdx.z * blockDim.y + threadIdx.y) * blockDim.x + threadIdx.x; i < (int)blockDim.z * pairs; i += n) {
                 const int z = blockDim.z == 1 ? 0 : i / pairs;
-                const int64_t tk = (int64_t)blockIdx.x * blockDim.z + z;
-                if (tk < tokens) table[i] = turn_of(a, (int)(tk / a.T), (int)(tk % a.T), i - z * pairs);
+                const uint32_t tk = blockIdx.x * blockDim.z + (uint32_t)z;
+                if (tk < tokens) table[i] = turn_of(a, (int)(tk / (uint32_t)a.T), (int)(tk % (uint32_t)a.T), i - z * pairs);
             }
             __syncthreads();
             if (turns)
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(MAX_THREADS) rotary_vec_kernel(const RotaryArg
 // any size and alignment: a block per token; thread-strided over (head, pair or copied channel)
 __global__ void __launch_bounds__(MAX_THREADS) rotary_kernel(const RotaryArgs a) {
     extern __shared__ float2 table[];                        // of the token's pairs
-    const int b = (int)(blockIdx.x / a.T), t = (int)(blockIdx.x % a.T), pairs = a.R / 2, work = pairs + a.D - a.R;
+    const int b = (int)(blockIdx.x / (uint32_t)a.T), t = (int)(blockIdx.x % (uint32_t)a.T), pairs = a.R / 2, work = pairs + a.D - a.R;
     for (int i = threadIdx.x; i < pairs; i += blockDim.x) table[i] = turn_of(a, b, t, i);
     __syncthreads();
     for (int64_t i = threadIdx.x; i < (int64_t)a.H * work; i += blockDim.x) {
