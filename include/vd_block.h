@@ -25,8 +25,8 @@ extern "C" {
  * Attention of many heads to states of another length:
  *   o[b,t,h,:] = sum_{u < len[b]} softmax_u(scale * q[b,t,h,:].k[b,u,h/g,:]) v[b,u,h/g,:],   g = heads / kv_heads
  * len = kv_lens clamped to 0..kv_len, or kv_len where kv_lens is NULL.  Keys and values at or behind len are never used,
- * whatever they hold; a row without keys is zeros.  Sums and the softmax are fp32; VD_BF16 rounds the probabilities
- * (relative to the row's largest) and the result to bf16.  Bitwise reproducible.
+ * whatever they hold; a row without keys is zeros.  Sums and the softmax are fp32; VD_BF16 rounds the result
+ * to bf16 and may round the probabilities (relative to the row's largest).  Bitwise reproducible.
  * ---------------------------------------------------------------------------------------- */
 typedef enum {
     VD_XATTN_AUTO = 0,

@@ -70,8 +70,8 @@ vd_status vd_op_cross_attention(const vd_xattn_desc* d, const void* q, const voi
     const int64_t rows = (int64_t)d->q_len * (d->heads / d->kv_heads);       // of a key head
     cudaError_t e;
     if (d->impl == VD_XATTN_AUTO && rows <= (d->dtype == VD_BF16 ? 16 : 4) && xattn_rows_supported(a)) e = launch_xattn_rows(a, (cudaStream_t)cuda_stream);
-    else if (d->impl == VD_XATTN_AUTO && xattn_f32_supported(a)) e = launch_xattn_f32(a, (cudaStream_t)cuda_stream);
-    else if (d->impl == VD_XATTN_AUTO && xattn_tc_supported(a)) e = launch_xattn_tc(a, (cudaStream_t)cuda_stream);
+    else if (d->impl == VD_XATTN_AUTO && d->dtype == VD_BF16 && xattn_tc_supported(a)) e = launch_xattn_tc(a, (cudaStream_t)cuda_stream);
+    else if (d->impl == VD_XATTN_AUTO) e = launch_xattn_f32(a, (cudaStream_t)cuda_stream);
     else e = launch_xattn_plain(a, (cudaStream_t)cuda_stream);
     return done(e, "vd_op_cross_attention");
 }

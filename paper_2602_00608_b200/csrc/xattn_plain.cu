@@ -1,7 +1,7 @@
 // Attention to states of another length, the kernel without restrictions: any head size up to 256, any strides and alignment.
 // A warp takes one row (batch item, token, head) and walks the keys one by one, running maximum and sum as in
 //   m' = max(m, s),  l' = l 2^(m - m') + 2^(s - m'),  o' = o 2^(m - m') + 2^(s - m') v.
-// Lane i holds channels i, i + 32, ... of q and o.  Scores are in units of log 2.
+// Lane i holds channels i, i + 32, ... of q and o.  Scores are in units of log 2.  The others are checked against it: nothing is shared with them.
 #include "block_ops.h"
 
 namespace vd {

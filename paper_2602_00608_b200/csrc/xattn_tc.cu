@@ -5,11 +5,16 @@
 // thread.  The two tiles take every block of 128 keys from shared memory together, and while one is in its softmax the tensor core
 // works for the other:
 //   S = Q K^T      K as it lies in memory, K-major
-//   softmax        running maximum with lazy rescaling of the output accumulator; exponentials partly on the FMA pipes (the special
-//                  function unit makes 16 a clock, 128 keys x 256 rows of them take as long as the products of 128 channels);
-//                  P in bf16 back to tensor memory, over S
+//   softmax        running maximum with lazy rescaling of the output accumulator (by powers of two, exactly); P in bf16 back to tensor memory,
+//                  a half at a time, so that the second half's exponentials overlap the first half's product
 //   O += P V       P from tensor memory, V as it lies in memory (MN-major): nothing is transposed
-// CTAs are persistent, one per SM; the next item's Q, K and scores are under way during an item's last rows.
+// CTAs are persistent, one per SM (contexts of one tile: two); the next item's Q, K and scores are under way during an item's last rows.
+// Rounded to bf16 are P (a half step, 2^-9 of a value, as the operand type asks) and the output; S, O, maxima and sums are fp32.
+// What bounds it.  A tile of 128 rows x 128 keys with heads of 128 takes the tensor core 1024 clocks (4096 multiply-adds each) and the special
+// function units as many (16 exponentials each): 9472 x 8192, 16 heads 477 us in a burst, 1330 TFLOP/s of the 1625 that a large matrix
+// product reaches, tensor pipe 62 % busy (4096 keys); run for long, the board's power holds back both (5400 x 14400 1060 TFLOP/s of 1397).
+// Heads of 64 halve the products and leave the exponentials: 8 x 1350 x 1350, 30 heads 192 us, special function units 63 % busy, the rest the
+// chain of scores, maximum, exponentials and product, which two tiles overlap and tensor memory has no room for a third.
 // Keys behind a row's length: scores are replaced before the maximum, P is zero there, and the up to 15 rows of V that the last
 // product still reads are zeroed in shared memory, since 0 * NaN is NaN.
 // Every wait is bounded (see tc_common.cuh); rows of an item whose wait gave up are NaN.
@@ -31,7 +36,9 @@ constexpr int HALF = KEYS / 2;                               // keys of P that g
 constexpr int SOFTMAX_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, NUM_THREADS = 352;     // MMA_WARP + s issues for tile s
 constexpr int MAX_LENS = 128;                                // lengths that are kept in shared memory
 constexpr int MAX_SPLITS = xa::MAX_SPLITS;
-constexpr double MEET_REST = 8.0, MEET_ALL = 5.0;            // what a meeting costs, in tiles
+// What a meeting costs, in tiles, by the loops and with all loads under way (18000 clocks; a tile is 2000 to 3000).  Dividing: 2 x 300 x 3000, 8 heads of
+// 128 49 -> 33 us; 5400 x 14400, 16 heads (352 items on 148 SMs: 2 rounds and a rest instead of 3) 596 -> 523; 9472 x 8192, 16 heads of 64 469 -> 453.
+constexpr double MEET_REST = 8.0, MEET_ALL = 5.0;
 constexpr float RESCALE_THRESHOLD = 8.0f;                    // log2 units: accumulators may grow by 2^8
 
 template <int DP, bool SHORT = false> struct Cfg {
@@ -43,9 +50,6 @@ template <int DP, bool SHORT = false> struct Cfg {
     static constexpr bool APART = DP == 64;
     static constexpr uint32_t TMEM = SHORT ? 256 : 512, P_COL = APART && !SHORT ? 384 : 0, P_STEP = APART && !SHORT ? 64 : 128;
     static constexpr uint32_t O_COL = SHORT ? 64 : 256, O_STEP = SHORT ? 128 : DP;
-    // every so many pairs of exponentials one on the FMA pipes; 0: none.  (They take five instructions for one, and where the products are
-    // short the issue slots are what is short.)
-    static constexpr int POLY = APART ? 0 : 16;
     static constexpr int MMA_WARPS = APART ? 2 : 1;
     static constexpr int SMEM = (Q_BUFS * 2 + 2 + STAGES) * TILE_BYTES + 2 * ROWS * 8 + MAX_LENS * 4 + 320;     // Q, O on its way out, K and V; (reference, sum) of the rows
 };
@@ -225,7 +229,6 @@ template <int DP> struct Tile {
     // of the exponentials, and the first half of P goes to the tensor core while the second one is made.  Returns the tile's maximum, NaN if
     // a score is.
     __device__ __forceinline__ float full(uint64_t* first_half) {
-        constexpr int POLY = Cfg<DP>::POLY;
         uint32_t a[32], b[32], c[32];
         tmem_ld32(t_s, a);
         tmem_ld32(t_s + 32u, b);
@@ -236,9 +239,9 @@ template <int DP> struct Tile {
         move_reference(t0 * scale_log2, 0u);
         const unsigned long long sc = pack2(scale_log2, scale_log2);
         unsigned long long mr = minus_ref();
-        exp_chunk<POLY>(a, t_p, sc, mr, sum, sum_b);
+        exp_chunk<0>(a, t_p, sc, mr, sum, sum_b);
         tmem_ld32(t_s + 96u, a);
-        exp_chunk<POLY>(b, t_p + 16u, sc, mr, sum, sum_b);
+        exp_chunk<0>(b, t_p + 16u, sc, mr, sum, sum_b);
         tmem_ld_wait();
         if (s_free) hand_over(s_free, lane);
         const float t1 = max_of(a, max_of(c, t0));
@@ -246,11 +249,13 @@ template <int DP> struct Tile {
         tmem_st_wait();
         hand_over(first_half, lane);
         mr = minus_ref();
-        exp_chunk<POLY>(c, t_p + 32u, sc, mr, sum, sum_b);
-        exp_chunk<POLY>(a, t_p + 48u, sc, mr, sum, sum_b);
+        exp_chunk<0>(c, t_p + 32u, sc, mr, sum, sum_b);
+        exp_chunk<0>(a, t_p + 48u, sc, mr, sum, sum_b);
         return t1;
     }
     // The same where only the first `valid` <= 96 keys count: the others leave before the maximum, 16 keys are the least that is worked on.
+    // A quarter of the exponentials on the FMA pipes (five instructions for one): this is a context's last tile, which little overlaps (8 x 1350 x 1350,
+    // 30 heads of 64 194.8 -> 192; in full() a 16th made no difference, an 8th was slower).
     __device__ __forceinline__ float most(int valid, uint64_t* first_half) {
         constexpr int POLY = 4;
         uint32_t a[32], b[32], c[32];
@@ -404,7 +409,7 @@ __device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
 // The CTAs of a cluster have each taken a share of an item's keys: they show one another half of the channels at a time, in fp32, and each
 // adds up (in the order of the shares) and writes its part of the tile's rows.  By the 128 threads of tile s; `rounds` counts what these
 // have shown so far.  A load of another CTA's memory takes 900 cycles.  FAST: a thread has a row, its weights in registers and all shares'
-// loads under way at once (18000 instead of 29000 cycles a meeting, 2 x 300 x 3000, 8 heads of 128, 36 -> 29 us), which crowds the softmax's
+// loads under way at once (18000 instead of 29000 cycles a meeting), which crowds the softmax's
 // registers: calls with whole items besides take the loops, out of line (5400 x 14400, 16 heads of 128 519 us, FAST 546).
 template <int DP, bool FAST>
 __device__ __forceinline__ void meet_inline(const Params& a, const Items<true>& it, Bars* bars, uint8_t* show, float2* ml, float2 mine, uint32_t t_o, int s, int row, uint32_t rounds) {

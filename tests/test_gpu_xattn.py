@@ -279,3 +279,28 @@ def test_short_contexts_of_many_items(vd, size):
     again = vd.op_cross_attention(q, k, v, lens, scale=scale)
     torch.cuda.synchronize()
     assert torch.equal(first.view(torch.int16), again.view(torch.int16))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [(2, 150, 400, 4, 2, 64), (1, 70, 5000, 2, 1, 100), (3, 3, 900, 6, 2, 250), (2, 130, 300, 2, 2, 192), (2, 2, 300, 130, 1, 64), (1, 1, 2000, 2, 2, 33),
+                                  (1, 700, 130, 20, 20, 128)], ids=lambda s: "x".join(map(str, s)))
+def test_any_alignment_and_width(vd, dtype, size):
+    """Heads that start at odd elements of odd rows, outputs too; ragged lengths with NaN behind them; what lies around the output stays."""
+    import torch
+    b, tq, tk, h, hkv, d = size
+    q, k, v = make(dtype, *size, seed=13)
+    lens = [tk, 0, tk // 2 + 1][:b]
+    for i, n in enumerate(lens):
+        k[i, n:], v[i, n:] = math.nan, math.nan
+    clean = [x.nan_to_num() for x in (k, v)]
+    wide = []
+    for x in (q, k, v, q):
+        w = torch.full((*x.shape[:3], d + 3), 7.0, dtype=x.dtype, device="cuda")
+        w[..., 1:1 + d] = x
+        wide.append(w)
+    dev = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    at = [w[..., 1:1 + d] for w in wide]
+    vd.op_cross_attention(*at[:3], dev, scale=d ** -0.5, out=at[3])
+    torch.cuda.synchronize()
+    block_ref.check(at[3], *block_ref.attention(q, *clean, dev, d ** -0.5))
+    assert (wide[3][..., 0] == 7).all() and (wide[3][..., 1 + d:] == 7).all()
