@@ -31,9 +31,9 @@ inline bool encode_kv(CUtensorMap* tm, const XAttnArgs& a, const void* p, const 
     return stride_ok(s.token, dims[1], &st[0]) && stride_ok(s.head, dims[2], &st[1]) && stride_ok(s.batch, dims[3], &st[2]) && encode_map(tm, p, 4, dims, st, box);
 }
 // strides, sizes and addresses that the maps of k and v can hold
-inline bool kv_maps_supported(const XAttnArgs& a) {
+inline bool kv_maps_supported(const XAttnArgs& a, int most_channels) {
     uint64_t unused;
-    return a.dtype == VD_BF16 && a.D % 8 == 0 && a.D <= 128 && a.Tk >= 1 && (((uintptr_t)a.k | (uintptr_t)a.v) & 15) == 0 &&
+    return a.dtype == VD_BF16 && a.D % 8 == 0 && a.D <= most_channels && a.Tk >= 1 && (((uintptr_t)a.k | (uintptr_t)a.v) & 15) == 0 &&
            stride_ok(a.sk.token, a.Tk, &unused) && stride_ok(a.sv.token, a.Tk, &unused) &&
            (a.sk.head == 0 || stride_ok(a.sk.head, a.Hkv, &unused)) && (a.sv.head == 0 || stride_ok(a.sv.head, a.Hkv, &unused)) &&
            (a.sk.batch == 0 || stride_ok(a.sk.batch, a.B, &unused)) && (a.sv.batch == 0 || stride_ok(a.sv.batch, a.B, &unused));

@@ -446,7 +446,7 @@ cudaError_t launch_xattn_rows(const XAttnArgs& a, cudaStream_t s) {
         // One row: few heads with long contexts want the ring's bytes in flight, many heads have them anyway and short contexts end
         // sooner without it (us, lanes / ring: 16 heads x 16000 keys of 64 23.5 / 16.6, 4 x 8000 of 128, 4 rows 33.7 / 12.5; 256 x 2000 43.1 / 45.4,
         // 32 x 100 4.8 / 6.5).  Two to four rows: 256 x 2000, two rows 48.0 / 45.8, 32 x 16384, four rows 103 / 47.
-        if ((rows > 1 || (a.Tk > 1024 && (int64_t)a.B * a.Hkv < 148)) && kv_maps_supported(a)) {
+        if ((rows > 1 || (a.Tk > 1024 && (int64_t)a.B * a.Hkv < 148)) && kv_maps_supported(a, 128)) {
             if (a.D <= 64) return rows <= 8 ? launch_stream<64, 1>(a, s) : launch_stream<64, 2>(a, s);
             return rows <= 8 ? launch_stream<128, 1>(a, s) : launch_stream<128, 2>(a, s);
         }

@@ -1,4 +1,4 @@
-// Attention to states of another length on tcgen05/TMEM (bf16, heads of up to 128 channels):
+// Attention to states of another length on tcgen05/TMEM (bf16, heads of up to 256 channels):
 //   o[b,t,h] = sum_{u < len[b]} softmax_u(scale q[b,t,h].k[b,u,h/g]) v[b,u,h/g]
 // An item is up to 256 rows of one key head: two tiles of 128 rows (a row is a token and one of the g heads that share the key head,
 // packed by the tensor map), each with a warpgroup of its own, one thread per row, so that a row's maximum and sum need no other
@@ -8,6 +8,8 @@
 //   softmax        running maximum with lazy rescaling of the output accumulator (by powers of two, exactly); P in bf16 back to tensor memory,
 //                  a half at a time, so that the second half's exponentials overlap the first half's product
 //   O += P V       P from tensor memory, V as it lies in memory (MN-major): nothing is transposed
+// Heads beyond 128 channels: an item is one tile, whose products (2048 clocks) the softmax of half a tile at a time still overlaps: 9472 x 8192, 8
+// heads of 256 520 us, 1220 TFLOP/s (in tiles on the FP32 pipes 2000 x 3000 takes 1843 us, here 62); their keys are not divided.
 // CTAs are persistent, one per SM (contexts of one tile: two); the next item's Q, K and scores are under way during an item's last rows.
 // Rounded to bf16 are P (a half step, 2^-9 of a value, as the operand type asks) and the output; S, O, maxima and sums are fp32.
 // What bounds it.  A tile of 128 rows x 128 keys with heads of 128 takes the tensor core 1024 clocks (4096 multiply-adds each) and the special
@@ -44,20 +46,22 @@ constexpr float RESCALE_THRESHOLD = 8.0f;                    // log2 units: accu
 template <int DP, bool SHORT = false> struct Cfg {
     static constexpr int CHUNKS = DP / CHUNK;
     static constexpr int TILE_BYTES = ROWS * DP * 2;         // of Q (a tile), K or V
-    static constexpr int STAGES = SHORT ? 2 : DP == 128 ? 3 : 6, Q_BUFS = SHORT || DP == 128 ? 1 : 2, CTAS = SHORT ? 2 : 1;     // CTAS of an SM
+    static constexpr int TILES = DP == 256 ? 1 : 2;          // of an item: tensor memory has no room for two O of 256 channels
+    static constexpr int STAGES = SHORT || DP == 256 ? 2 : DP == 128 ? 3 : 6, Q_BUFS = SHORT || DP > 64 ? 1 : 2;
+    static constexpr bool O_OVER_Q = DP == 256;              // shared memory has none for O on its way out: it takes Q's place
     // Tensor memory has room for a P of its own beside the scores where O takes 64 columns: the next scores then do not wait for the
     // products of P.  Columns of tile s: S at 128 s, O at O_COL + O_STEP s, P at P_COL + P_STEP s.  SHORT: the second half of S is O's.
     static constexpr bool APART = DP == 64;
     static constexpr uint32_t TMEM = SHORT ? 256 : 512, P_COL = APART && !SHORT ? 384 : 0, P_STEP = APART && !SHORT ? 64 : 128;
     static constexpr uint32_t O_COL = SHORT ? 64 : 256, O_STEP = SHORT ? 128 : DP;
     static constexpr int MMA_WARPS = APART ? 2 : 1;
-    static constexpr int SMEM = (Q_BUFS * 2 + 2 + STAGES) * TILE_BYTES + 2 * ROWS * 8 + MAX_LENS * 4 + 320;     // Q, O on its way out, K and V; (reference, sum) of the rows
+    static constexpr int SMEM = (Q_BUFS * TILES + (O_OVER_Q ? 0 : TILES) + STAGES) * TILE_BYTES + 2 * ROWS * 8 + MAX_LENS * 4 + 320;     // Q, O on its way out, K and V; (reference, sum) of the rows
 };
 struct Bars {
-    uint64_t q_full[2], q_empty[2], full[6], empty[6], s_full[2], s_free[2], p_part[2][2], pv_done[2], o_full[2], drained[2], shown[2], seen[2];
+    uint64_t q_full[2], q_empty[2], full[6], empty[6], s_full[2], s_free[2], p_part[2][2], pv_done[2], o_full[2], drained[2], shown[2], seen[2], o_left;
     uint32_t tmem_base, abort_flag;
 };
-static_assert(sizeof(Bars) <= 320 && Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448 && 2 * (Cfg<64, true>::SMEM + 1024) <= 233472, "shared memory of one CTA");
+static_assert(sizeof(Bars) <= 320 && Cfg<256>::SMEM <= 232448 && Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448 && 2 * (Cfg<64, true>::SMEM + 1024) <= 233472, "shared memory of one CTA");
 
 struct Params {
     const int32_t* lens;
@@ -348,7 +352,7 @@ template <int DP> struct Tile {
 };
 
 // A CTA's items: of the whole ones those one grid apart (no divisions on the way), then its share of the keys of its cluster's.
-template <bool SPLIT> struct Items {
+template <bool SPLIT, int TILES = 2> struct Items {
     int b, kvh, qt, t0, streams, len, tiles;     // tiles of the item, of which [j0, j0 + n) are this CTA's
     int j0, n;
     uint32_t at;
@@ -379,8 +383,8 @@ template <bool SPLIT> struct Items {
             place(a);
         }
         if (at >= a.items) return false;
-        t0 = qt * 2 * a.nt;
-        streams = t0 + a.nt < a.Tq ? 2 : 1;
+        t0 = qt * TILES * a.nt;
+        streams = TILES == 2 && t0 + a.nt < a.Tq ? 2 : 1;
         len = !a.lens ? a.Tk : min(max(b < MAX_LENS ? lens[b] : a.lens[b], 0), a.Tk);
         tiles = (len + KEYS - 1) / KEYS;
         j0 = 0;
@@ -531,8 +535,8 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
     using C = Cfg<DP, ONE_TILE>;
     extern __shared__ __align__(1024) uint8_t smem_q[];
     if (smem_u32(smem_q) & 1023u) return;                    // (it is: the swizzle needs it)
-    uint8_t* smem_o = smem_q + C::Q_BUFS * 2 * C::TILE_BYTES;
-    uint8_t* smem_st = smem_o + 2 * C::TILE_BYTES;
+    uint8_t* smem_o = smem_q + (C::O_OVER_Q ? 0 : C::Q_BUFS * C::TILES * C::TILE_BYTES);
+    uint8_t* smem_st = smem_o + C::TILES * C::TILE_BYTES;
     float2* ml = (float2*)(smem_st + C::STAGES * C::TILE_BYTES);         // [2][ROWS]
     int* lens = (int*)(ml + 2 * ROWS);
     Bars* bars = (Bars*)(lens + MAX_LENS);
@@ -547,6 +551,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
             mbar_init(smem_u32(&bars->shown[i]), (uint32_t)a.splits); mbar_init(smem_u32(&bars->seen[i]), (uint32_t)a.splits);
         }
         for (int i = 0; i < C::STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), C::MMA_WARPS); }
+        mbar_init(smem_u32(&bars->o_left), 1);
         bars->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async_smem();
@@ -567,7 +572,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
         const bool out_thread = (tid & (ROWS - 1)) == 0;
         uint32_t n_s = 0, n_o = 0, n_pv = 0, n_meet = 0;     // tiles, items, waited-for products and rounds of meetings so far
         bool ok = true;
-        for (Items<SPLIT> it(a); it.take(a, lens);) {
+        for (Items<SPLIT, C::TILES> it(a); it.take(a, lens);) {
             if (s >= it.streams || (SPLIT && it.split && it.tiles == 0 && blockIdx.x % (uint32_t)a.splits != 0)) continue;
             float m_ref = -INFINITY;
             unsigned long long sum = 0, sum_b = 0;           // of even and odd pairs of keys
@@ -640,9 +645,13 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
             fence_proxy_async_smem();
             named_barrier_sync(1 + s, ROWS);
             if (out_thread) {
-                for (int c = 0; c < C::CHUNKS; ++c)
+                for (int c = 0; c < C::CHUNKS && c * CHUNK < a.D; ++c)
                     tma_store_5d(&tm_o, smem_u32(smem_o + s * C::TILE_BYTES + c * (ROWS * 128)), c * CHUNK, 0, it.t0 + s * a.nt, it.kvh, it.b);
                 bulk_commit_group();
+                if (C::O_OVER_Q) {
+                    bulk_wait_group_read<0>();
+                    mbar_arrive(smem_u32(&bars->o_left));
+                }
             }
             tc_fence_before();                               // (the next product into O waits for this warp's next P)
         }
@@ -651,9 +660,11 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
         // ------------------------------------------------------------ loads: Q, then K and V of each tile in turn
         if (lane == 0) {
             uint32_t st = 0, ph = 0;
-            int issued = 0, q_issued = 0;
+            int issued = 0, q_issued = 0, items = 0;
             bool ok = true;
-            for (Items<SPLIT> it(a); ok && it.take(a, lens);) {
+            for (Items<SPLIT, C::TILES> it(a); ok && it.take(a, lens);) {
+                if (C::O_OVER_Q && items++ > 0) ok = mbar_wait(smem_u32(&bars->o_left), items & 1, abort_flag);
+                if (!ok) break;
                 if (!it.n) continue;
                 const int buf = q_issued % C::Q_BUFS;
                 ok = mbar_wait(smem_u32(&bars->q_empty[buf]), ((q_issued / C::Q_BUFS) & 1) ^ 1, abort_flag);
@@ -744,7 +755,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
         if constexpr (C::APART) {
             const int s = warp - MMA_WARP;
             uint32_t n_p = 0, n_f = 0;
-            for (Items<SPLIT> it(a); it.take(a, lens);) {
+            for (Items<SPLIT, C::TILES> it(a); it.take(a, lens);) {
                 if (!it.n) continue;
                 if (*abort_flag) break;
                 wait_on(&bars->q_full[n_q % C::Q_BUFS], (n_q / C::Q_BUFS) & 1);
@@ -794,7 +805,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
             }
         } else {
             uint32_t n_p[2] = {0, 0};
-            for (Items<SPLIT> it(a); it.take(a, lens);) {
+            for (Items<SPLIT, C::TILES> it(a); it.take(a, lens);) {
                 if (!it.n) continue;
                 if (*abort_flag) break;
                 wait_on(&bars->q_full[n_q % C::Q_BUFS], (n_q / C::Q_BUFS) & 1);
@@ -888,22 +899,30 @@ template <int DP> cudaError_t launch(Params& p, const CUtensorMap& tq, const CUt
         p.db = (int)(heads / (uint32_t)p.Hkv);
         return grid;
     };
-    if constexpr (DP == 64)
-        if (p.Tk <= KEYS) {
-            constexpr int short_smem = Cfg<DP, true>::SMEM;
-            p.splits = 1;
-            p.whole = p.items;
-            const uint32_t grid = step(std::min(p.items, 2u * (uint32_t)sms));
-            return cc::launch_clusters<xattn_tc_kernel<DP, SHORT>>({grid, NUM_THREADS, short_smem, short_smem, 1}, s, p, tq, tk, tv, to);
-        }
-    constexpr int smem = Cfg<DP>::SMEM;
-    const Division d = divide<DP>(p.items, p.Tk, sms);
-    p.splits = d.splits;
-    p.whole = d.whole;
-    const uint32_t grid = step(d.grid);
-    if (p.splits > 1 && p.whole) return cc::launch_clusters<xattn_tc_kernel<DP, REST>>({grid, NUM_THREADS, smem, smem, p.splits}, s, p, tq, tk, tv, to);
-    if (p.splits > 1) return cc::launch_clusters<xattn_tc_kernel<DP, ALL>>({grid, NUM_THREADS, smem, smem, p.splits}, s, p, tq, tk, tv, to);
-    return cc::launch_clusters<xattn_tc_kernel<DP, NONE>>({grid, NUM_THREADS, smem, smem, 1}, s, p, tq, tk, tv, to);
+    if constexpr (DP == 256) {
+        constexpr int smem = Cfg<DP>::SMEM;
+        p.splits = 1;
+        p.whole = p.items;
+        const uint32_t grid = step(std::min(p.items, (uint32_t)sms));
+        return cc::launch_clusters<xattn_tc_kernel<DP, NONE>>({grid, NUM_THREADS, smem, smem, 1}, s, p, tq, tk, tv, to);
+    } else {
+        if constexpr (DP == 64)
+            if (p.Tk <= KEYS) {
+                constexpr int short_smem = Cfg<DP, true>::SMEM;
+                p.splits = 1;
+                p.whole = p.items;
+                const uint32_t grid = step(std::min(p.items, 2u * (uint32_t)sms));
+                return cc::launch_clusters<xattn_tc_kernel<DP, SHORT>>({grid, NUM_THREADS, short_smem, short_smem, 1}, s, p, tq, tk, tv, to);
+            }
+        constexpr int smem = Cfg<DP>::SMEM;
+        const Division d = divide<DP>(p.items, p.Tk, sms);
+        p.splits = d.splits;
+        p.whole = d.whole;
+        const uint32_t grid = step(d.grid);
+        if (p.splits > 1 && p.whole) return cc::launch_clusters<xattn_tc_kernel<DP, REST>>({grid, NUM_THREADS, smem, smem, p.splits}, s, p, tq, tk, tv, to);
+        if (p.splits > 1) return cc::launch_clusters<xattn_tc_kernel<DP, ALL>>({grid, NUM_THREADS, smem, smem, p.splits}, s, p, tq, tk, tv, to);
+        return cc::launch_clusters<xattn_tc_kernel<DP, NONE>>({grid, NUM_THREADS, smem, smem, 1}, s, p, tq, tk, tv, to);
+    }
 }
 
 }  // namespace
@@ -915,7 +934,7 @@ bool xattn_tc_supported(const XAttnArgs& a) {
         return ((uintptr_t)p & 15) == 0 && stride_ok(s.head, a.H, &unused) && stride_ok(s.token, a.Tq, &unused) && stride_ok(s.batch, a.B, &unused) &&
                s.head < (1ll << 38) / std::max(g, 1);
     };
-    return kv_maps_supported(a) && g <= ROWS && rows_ok(a.q, a.sq) && rows_ok(a.o, a.so);
+    return kv_maps_supported(a, 256) && g <= ROWS && rows_ok(a.q, a.sq) && rows_ok(a.o, a.so);
 }
 
 cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s) {
@@ -924,7 +943,8 @@ cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s) {
     p.o = (__nv_bfloat16*)a.o; p.o_batch = a.so.batch; p.o_token = a.so.token; p.o_head = a.so.head;
     p.lens = a.kv_lens;
     p.Tq = a.Tq; p.Tk = a.Tk; p.B = a.B; p.Hkv = a.Hkv; p.g = a.H / a.Hkv; p.D = a.D; p.nt = ROWS / p.g;
-    p.q_items = (a.Tq + 2 * p.nt - 1) / (2 * p.nt);
+    const int tokens = (a.D > 128 ? 1 : 2) * p.nt;           // of an item
+    p.q_items = (a.Tq + tokens - 1) / tokens;
     p.items = (uint32_t)((int64_t)p.q_items * a.Hkv * a.B);          // (rows are at most 2^30)
     p.scale_log2 = a.scale * 1.4426950408889634f;
     if (!encode_rows(&tq, a, a.q, a.sq, p.nt) || !encode_rows(&to, a, a.o, a.so, p.nt) || !encode_kv(&tk, a, a.k, a.sk, KEYS, &p.kh, &p.kb) ||
@@ -934,7 +954,8 @@ cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
-    return a.D <= 64 ? launch<64>(p, tq, tk, tv, to, sms, s) : launch<128>(p, tq, tk, tv, to, sms, s);
+    if (a.D <= 64) return launch<64>(p, tq, tk, tv, to, sms, s);
+    return a.D <= 128 ? launch<128>(p, tq, tk, tv, to, sms, s) : launch<256>(p, tq, tk, tv, to, sms, s);
 }
 
 }  // namespace vd

@@ -304,3 +304,26 @@ def test_any_alignment_and_width(vd, dtype, size):
     torch.cuda.synchronize()
     block_ref.check(at[3], *block_ref.attention(q, *clean, dev, d ** -0.5))
     assert (wide[3][..., 0] == 7).all() and (wide[3][..., 1 + d:] == 7).all()
+
+
+@pytest.mark.parametrize("size", [(1, 130, 260, 3, 3, 256), (3, 140, 300, 4, 2, 192), (5, 300, 129, 2, 1, 136), (40, 257, 130, 10, 10, 256), (2, 700, 1500, 6, 2, 200), (30, 40, 600, 24, 12, 256)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_wide_heads(vd, size):
+    """Beyond 128 channels: every length from none to all, NaN behind each, scores that grow from tile to tile, the same bits again."""
+    import torch
+    b, _, tk = size[:3]
+    q, k, v = make("bf16", *size, seed=14)
+    k *= 1 + 8 * torch.arange(tk, device="cuda", dtype=k.dtype)[None, :, None, None] / tk
+    lens = torch.tensor([tk - (i * tk) // max(1, b - 1) if b > 2 else tk - i for i in range(b)], dtype=torch.int32, device="cuda")
+    behind = torch.arange(tk, device="cuda")[None, :, None, None] >= lens[:, None, None, None]
+    scale = q.shape[3] ** -0.5
+    want = block_ref.attention(q, k.masked_fill(behind, 0), v.masked_fill(behind, 0), lens, scale)
+    k.masked_fill_(behind, math.nan)
+    v.masked_fill_(behind, math.nan)
+    first = vd.op_cross_attention(q, k, v, lens, scale=scale)
+    torch.cuda.synchronize()
+    block_ref.check(first, *want)
+    assert (first[lens == 0] == 0).all()
+    again = vd.op_cross_attention(q, k, v, lens, scale=scale)
+    torch.cuda.synchronize()
+    assert torch.equal(first.view(torch.int16), again.view(torch.int16))
