@@ -623,6 +623,7 @@ def op_cross_attention(q, k, v, kv_lens=None, scale=None, out=None, impl=VD_XATT
         if status != VD_OK:
             _check(status)
         return out
+    scale, impl = None if scale is None else float(scale), int(impl)         # (what is kept is keyed by values, never by an object)
     desc = _described(("xattn", scale, impl, _sig(q), _sig(k), _sig(v), _sig(kv_lens), _sig(out)), _describe_cross_attention,
                       q, k, v, kv_lens, scale, out, impl)
     _launch(q, lib().vd_op_cross_attention, byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(kv_lens), out.data_ptr())
@@ -693,6 +694,8 @@ def op_rotary(x, freqs, positions=None, *, layout="half", axis_pairs=None, ampli
         if status != VD_OK:
             _check(status)
         return out
+    amplitude, first_position = float(amplitude), int(first_position)
+    axis_pairs = None if axis_pairs is None else tuple(int(n) for n in axis_pairs)
     desc = _described(("rotary", layout, axis_pairs, amplitude, first_position, _sig(x), _sig(freqs), _sig(positions), _sig(out)), _describe_rotary,
                       x, freqs, positions, layout, axis_pairs, amplitude, first_position, out)
     _launch(x, lib().vd_op_rotary, byref(desc), x.data_ptr(), _ptr(positions), freqs.data_ptr(), out.data_ptr())
@@ -761,6 +764,7 @@ def op_gate_norm(x, h=None, *, gate=None, scale=None, shift=None, kind="layer", 
         if status != VD_OK:
             _check(status)
         return x_out, y
+    eps, post_norm, residual_scale, mod_tokens = float(eps), bool(post_norm), float(residual_scale), None if mod_tokens is None else int(mod_tokens)
     desc = _described(("norm", kind, eps, post_norm, residual_scale, mod_tokens, _sig(x), _sig(h), _sig(gate), _sig(scale), _sig(shift), _sig(weight), _sig(bias),
                        _sig(post_weight), _sig(x_out), _sig(y)), _describe_gate_norm,
                       x, h, gate, scale, shift, kind, eps, weight, bias, post_norm, post_weight, residual_scale, mod_tokens, x_out, y)

@@ -64,6 +64,7 @@ vd_status vd_op_cross_attention(const vd_xattn_desc* d, const void* q, const voi
     if (!q || !o || (d->kv_len > 0 && (!k || !v))) return refuse(VD_ERR_INVALID_ARG, "NULL pointer");
     if (!aligned_to(q, d->dtype) || !aligned_to(k, d->dtype) || !aligned_to(v, d->dtype) || !aligned_to(o, d->dtype) || ((uintptr_t)kv_lens & 3))
         return refuse(VD_ERR_INVALID_ARG, "misaligned pointer");
+    if (o == q || o == k || o == v) return refuse(VD_ERR_INVALID_ARG, "o is an input");
     XAttnArgs a{q, k, v, o, kv_lens, d->dtype, d->batch, d->q_len, d->kv_len, d->heads, d->kv_heads, d->head_dim,
                 {d->q_batch, d->q_token, d->q_head}, {d->k_batch, d->k_token, d->k_head}, {d->v_batch, d->v_token, d->v_head},
                 {d->o_batch, d->o_token, d->o_head}, d->scale};

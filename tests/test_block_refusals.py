@@ -187,3 +187,11 @@ def test_the_wrappers_refuse_sizes_that_would_wrap():
         with pytest.raises(vd.VdError) as e:
             call()
         assert e.value.status == vd.VD_ERR_INVALID_ARG and "device" not in str(e.value)
+
+
+@pytest.mark.parametrize("which", range(3))
+def test_cross_attention_refuses_an_output_that_is_an_input(which):
+    """Rows are read while others are written."""
+    at = [ctypes.c_void_p(4096 * (i + 1)) for i in range(3)]
+    assert vd.lib().vd_op_cross_attention(ctypes.byref(xattn()), *at, None, at[which], None) == vd.VD_ERR_INVALID_ARG
+    assert b"o is an input" in vd.lib().vd_last_error(None)

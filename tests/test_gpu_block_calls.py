@@ -104,3 +104,20 @@ def test_calls_take_the_current_stream(vd, monkeypatch, native):
         r, _ = vd.op_gate_norm(x, want_y=False)
     torch.cuda.synchronize()
     assert (r == 20).all()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_numbers_that_are_tensors_count_as_they_are_at_the_call(vd, monkeypatch, native):
+    import torch
+    if not native:
+        monkeypatch.setattr(vd, "_native", False)
+    g = torch.Generator(device="cuda").manual_seed(22)
+    q = torch.randn((1, 9, 2, 64), generator=g, device="cuda")
+    k, v, x = torch.randn_like(q), torch.randn_like(q), torch.randn((1, 9, 64), generator=g, device="cuda")
+    freqs, n = vd.rotary_frequencies(64).cuda(), torch.tensor(0.5)
+    calls = [lambda n: vd.op_cross_attention(q, k, v, scale=n), lambda n: vd.op_rotary(q, freqs, amplitude=n), lambda n: vd.op_gate_norm(x, x, residual_scale=n)[0],
+             lambda n: vd.op_gate_norm(x, eps=n)[1]]
+    for call in calls:
+        for value in (0.5, 0.125):
+            n.fill_(value)
+            assert torch.equal(call(n), call(value))
