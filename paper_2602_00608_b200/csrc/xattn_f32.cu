@@ -1,7 +1,8 @@
 // Attention to states of another length in single precision, on the FP32 pipes (no operand or sum in fewer bits; the tensor core
 // drops what falls off a running sum, and one of several hundred keys shows it), and of what the tensor core's kernel does not take:
-// heads of any width up to 256, any alignment and stride (2000 x 3000, 8 heads of 100, bf16: 626 us; a warp per row, xattn_plain.cu, 7608).  A CTA of 128 threads takes 16 RT rows of a key head
-// (a row: a token and one of the heads that share it) and walks blocks of 8 KJ keys; two CTAs share an SM, so that one computes
+// heads of any width up to 256, any alignment and stride (2000 x 3000, 8 heads of 100, bf16: 626 us; a warp per row, xattn_plain.cu, 7608).
+// A CTA of 128 threads takes 16 RT rows of a key head (a row: a token and one of the heads that share it) and walks blocks of 8 KJ keys;
+// two CTAs share an SM (one with heads beyond 128 channels), so that one computes
 // while the other exchanges.  What bounds it is the way from shared memory to the registers, 128 bytes a clock for all warps, broadcast or
 // not: an fma.rn.f32x2 of a thread may take two of a thread's bytes.  So a thread holds as much as its registers allow:
 //   scores   RT rows x KJ keys, pairs along the channels, so that both operands are pairs as they lie in memory.  Its keys are 8 apart and

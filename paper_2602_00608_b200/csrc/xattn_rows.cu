@@ -247,10 +247,10 @@ __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
 __device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-constexpr int STREAM_WARPS = 8, STREAM_KEYS = STREAM_WARPS * 16, STREAM_THREADS = (STREAM_WARPS + 1) * 32;
-template <int DP> struct StreamCfg {
-    static constexpr int STAGES = DP == 128 ? 3 : 6, TILE = STREAM_KEYS * DP * 2, SMEM = STAGES * 2 * TILE + 128 + 1024;
-    static_assert(SMEM <= 232448 && shared_bytes(STREAM_WARPS, 16, DP) <= STAGES * 2 * TILE, "shared memory of one CTA; the meeting's lies over the stages");
+template <int DP> struct StreamCfg {                         // (heads beyond 128 channels: half the keys a stage, so that three still fit)
+    static constexpr int WARPS = DP == 256 ? 4 : 8, KEYS = WARPS * 16, THREADS = (WARPS + 1) * 32;
+    static constexpr int STAGES = DP == 64 ? 6 : 3, TILE = KEYS * DP * 2, SMEM = STAGES * 2 * TILE + 128 + 1024;
+    static_assert(SMEM <= 232448 && shared_bytes(WARPS, 16, DP) <= STAGES * 2 * TILE, "shared memory of one CTA; the meeting's lies over the stages");
 };
 struct StreamBars { uint64_t full[6], empty[6]; uint32_t abort_flag; };
 static_assert(sizeof(StreamBars) <= 128, "");
@@ -260,10 +260,10 @@ struct StreamParams {
 };
 // NR: groups of eight rows
 template <int DP, int NR>
-__global__ void __launch_bounds__(STREAM_THREADS, 1)
+__global__ void __launch_bounds__(StreamCfg<DP>::THREADS, 1)
 xattn_stream_kernel(const StreamParams sp, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
     using C = StreamCfg<DP>;
-    constexpr int R = NR * 8, KS = DP / 16;
+    constexpr int R = NR * 8, KS = DP / 16, WARPS = C::WARPS, KEYS = C::KEYS;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* stages = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     StreamBars* bars = (StreamBars*)(stages + C::STAGES * 2 * C::TILE);
@@ -272,7 +272,7 @@ xattn_stream_kernel(const StreamParams sp, const __grid_constant__ CUtensorMap t
     const XAttnArgs& a = p.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     if (tid == 0) {
-        for (int i = 0; i < C::STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), STREAM_WARPS); }
+        for (int i = 0; i < C::STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), WARPS); }
         bars->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async_smem();
@@ -280,13 +280,13 @@ xattn_stream_kernel(const StreamParams sp, const __grid_constant__ CUtensorMap t
     __syncthreads();
     const int split = p.splits > 1 ? (int)cluster_ctarank() : 0;
     const Work w = work_of<R>(p);
-    const int tiles = (w.len + STREAM_KEYS - 1) / STREAM_KEYS, mine = tiles > split ? (tiles - split + p.splits - 1) / p.splits : 0;
-    const Shared<DP, STREAM_WARPS> sh((float*)stages, R);
+    const int tiles = (w.len + KEYS - 1) / KEYS, mine = tiles > split ? (tiles - split + p.splits - 1) / p.splits : 0;
+    const Shared<DP, WARPS> sh((float*)stages, R);
     float o[KS][NR][4] = {};                                 // channels 16 i + g, + 8 of rows 8 n + 2c, + 1
     float m[NR][2], l[NR][2];
 #pragma unroll
     for (int n = 0; n < NR; ++n) { m[n][0] = m[n][1] = -INFINITY; l[n][0] = l[n][1] = 0.f; }
-    if (warp == STREAM_WARPS) {
+    if (warp == WARPS) {
         if (lane == 0) {
             bool ok = true;
             int i = 0;
@@ -297,8 +297,8 @@ xattn_stream_kernel(const StreamParams sp, const __grid_constant__ CUtensorMap t
                 const uint32_t full = smem_u32(&bars->full[st]), dst = smem_u32(stages + st * 2 * C::TILE);
                 mbar_arrive_expect_tx(full, 2 * C::TILE);
                 for (int x = 0; x < DP / 64; ++x) {
-                    tma_load_4d(dst + x * (STREAM_KEYS * 128), &tm_k, x * 64, tile * STREAM_KEYS, w.kvh * sp.kh, w.b * sp.kb, full);
-                    tma_load_4d(dst + C::TILE + x * (STREAM_KEYS * 128), &tm_v, x * 64, tile * STREAM_KEYS, w.kvh * sp.vh, w.b * sp.vb, full);
+                    tma_load_4d(dst + x * (KEYS * 128), &tm_k, x * 64, tile * KEYS, w.kvh * sp.kh, w.b * sp.kb, full);
+                    tma_load_4d(dst + C::TILE + x * (KEYS * 128), &tm_v, x * 64, tile * KEYS, w.kvh * sp.vh, w.b * sp.vb, full);
                 }
             }
             if (!ok || *abort_flag) cc::land_loads(bars->full, C::STAGES, i);     // (else the others wait for all of them)
@@ -320,7 +320,7 @@ xattn_stream_kernel(const StreamParams sp, const __grid_constant__ CUtensorMap t
         const uint32_t k_at = (uint32_t)(k_row * 128), v_at = (uint32_t)(v_row * 128), k_hi = (uint32_t)(lane >> 4), v_hi = (uint32_t)((lane >> 3) & 1), sw = (uint32_t)(lane & 7);
         bool ok = true;
         for (int i = 0; i < mine; ++i) {
-            const int st = i % C::STAGES, left = w.len - (split + i * p.splits) * STREAM_KEYS - warp * 16;       // keys of this warp's 16 that count
+            const int st = i % C::STAGES, left = w.len - (split + i * p.splits) * KEYS - warp * 16;       // keys of this warp's 16 that count
             ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->full[st]), (i / C::STAGES) & 1, abort_flag)) && ok;
             if (left > 0) {
                 const uint32_t kt = smem_u32(stages + st * 2 * C::TILE) + k_at, vt = smem_u32(stages + st * 2 * C::TILE + C::TILE) + v_at;
@@ -328,7 +328,7 @@ xattn_stream_kernel(const StreamParams sp, const __grid_constant__ CUtensorMap t
                     for (int x = lane; x < (16 - left) * 8; x += 32)
 #pragma unroll
                         for (int y = 0; y < DP / 64; ++y)
-                            *(uint4*)(stages + st * 2 * C::TILE + C::TILE + y * (STREAM_KEYS * 128) + (warp * 16 + left) * 128 + x * 16) = make_uint4(0, 0, 0, 0);
+                            *(uint4*)(stages + st * 2 * C::TILE + C::TILE + y * (KEYS * 128) + (warp * 16 + left) * 128 + x * 16) = make_uint4(0, 0, 0, 0);
                     __syncwarp();
                 }
                 float s[NR][4], s1[NR][4];                   // keys g (first two) and g + 8 of rows 8 n + 2c, + 1
@@ -339,7 +339,7 @@ xattn_stream_kernel(const StreamParams sp, const __grid_constant__ CUtensorMap t
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
                     uint32_t f[4];
-                    ldsm4(f, kt + (uint32_t)((k >> 2) * (STREAM_KEYS * 128)) + (((uint32_t)((k & 3) * 2) + k_hi) ^ sw) * 16u);
+                    ldsm4(f, kt + (uint32_t)((k >> 2) * (KEYS * 128)) + (((uint32_t)((k & 3) * 2) + k_hi) ^ sw) * 16u);
 #pragma unroll
                     for (int n = 0; n < NR; ++n) mma_16816(k & 1 ? s1[n] : s[n], f, q[k][n][0], q[k][n][1]);
                 }
@@ -379,7 +379,7 @@ xattn_stream_kernel(const StreamParams sp, const __grid_constant__ CUtensorMap t
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
                     uint32_t f[4];
-                    ldsm4_t(f, vt + (uint32_t)((k >> 2) * (STREAM_KEYS * 128)) + (((uint32_t)((k & 3) * 2) + v_hi) ^ sw) * 16u);
+                    ldsm4_t(f, vt + (uint32_t)((k >> 2) * (KEYS * 128)) + (((uint32_t)((k & 3) * 2) + v_hi) ^ sw) * 16u);
 #pragma unroll
                     for (int n = 0; n < NR; ++n) mma_16816(o[k][n], f, b0[n], b1[n]);
                 }
@@ -390,7 +390,7 @@ xattn_stream_kernel(const StreamParams sp, const __grid_constant__ CUtensorMap t
         if (!ok) l[0][0] = l[0][1] = l[NR - 1][0] = l[NR - 1][1] = __int_as_float(0x7fffffff);
     }
     __syncthreads();                                         // every load has landed and been used: the stages become the meeting's memory
-    if (warp < STREAM_WARPS) {
+    if (warp < WARPS) {
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -405,7 +405,7 @@ xattn_stream_kernel(const StreamParams sp, const __grid_constant__ CUtensorMap t
                 }
             }
     }
-    meet<__nv_bfloat16, DP, STREAM_WARPS>(p, sh, w, split, tid);
+    meet<__nv_bfloat16, DP, WARPS>(p, sh, w, split, tid);
 }
 
 template <typename T, int R, int U, int LPK, int NVL> cudaError_t launch(const XAttnArgs& a, cudaStream_t s) {
@@ -414,12 +414,12 @@ template <typename T, int R, int U, int LPK, int NVL> cudaError_t launch(const X
     return cc::launch_clusters<xattn_rows_kernel<T, R, U, LPK, NVL, W>>({(int64_t)p.groups * a.Hkv * a.B * p.splits, W * 32, smem, smem, p.splits}, s, p);
 }
 template <int DP, int NR> cudaError_t launch_stream(const XAttnArgs& a, cudaStream_t s) {
-    constexpr int smem = StreamCfg<DP>::SMEM;
+    using C = StreamCfg<DP>;
     CUtensorMap tk, tv;
     StreamParams sp;
-    if (!encode_kv(&tk, a, a.k, a.sk, STREAM_KEYS, &sp.kh, &sp.kb) || !encode_kv(&tv, a, a.v, a.sv, STREAM_KEYS, &sp.vh, &sp.vb)) return cudaErrorInvalidValue;
-    sp.p = plan_rows<xattn_stream_kernel<DP, NR>>(a, STREAM_THREADS, NR * 8, smem, STREAM_KEYS);
-    return cc::launch_clusters<xattn_stream_kernel<DP, NR>>({(int64_t)sp.p.groups * a.Hkv * a.B * sp.p.splits, STREAM_THREADS, smem, smem, sp.p.splits}, s, sp, tk, tv);
+    if (!encode_kv(&tk, a, a.k, a.sk, C::KEYS, &sp.kh, &sp.kb) || !encode_kv(&tv, a, a.v, a.sv, C::KEYS, &sp.vh, &sp.vb)) return cudaErrorInvalidValue;
+    sp.p = plan_rows<xattn_stream_kernel<DP, NR>>(a, C::THREADS, NR * 8, C::SMEM, C::KEYS);
+    return cc::launch_clusters<xattn_stream_kernel<DP, NR>>({(int64_t)sp.p.groups * a.Hkv * a.B * sp.p.splits, C::THREADS, C::SMEM, C::SMEM, sp.p.splits}, s, sp, tk, tv);
 }
 
 template <typename T, int R> cudaError_t launch_rows(const XAttnArgs& a, cudaStream_t s) {
@@ -446,9 +446,11 @@ cudaError_t launch_xattn_rows(const XAttnArgs& a, cudaStream_t s) {
         // One row: few heads with long contexts want the ring's bytes in flight, many heads have them anyway and short contexts end
         // sooner without it (us, lanes / ring: 16 heads x 16000 keys of 64 23.5 / 16.6, 4 x 8000 of 128, 4 rows 33.7 / 12.5; 256 x 2000 43.1 / 45.4,
         // 32 x 100 4.8 / 6.5).  Two to four rows: 256 x 2000, two rows 48.0 / 45.8, 32 x 16384, four rows 103 / 47.
-        if ((rows > 1 || (a.Tk > 1024 && (int64_t)a.B * a.Hkv < 148)) && kv_maps_supported(a, 128)) {
+        // Heads of 256: 32 x 16384, one row 82 / 86, four 150 / 87, sixteen of 8000 keys 259 / 58; 4 x 500, two rows 8.3 / 10.6.
+        if ((rows > 1 || (a.D <= 128 && a.Tk > 1024 && (int64_t)a.B * a.Hkv < 148)) && kv_maps_supported(a, 256)) {
             if (a.D <= 64) return rows <= 8 ? launch_stream<64, 1>(a, s) : launch_stream<64, 2>(a, s);
-            return rows <= 8 ? launch_stream<128, 1>(a, s) : launch_stream<128, 2>(a, s);
+            if (a.D <= 128) return rows <= 8 ? launch_stream<128, 1>(a, s) : launch_stream<128, 2>(a, s);
+            return rows <= 8 ? launch_stream<256, 1>(a, s) : launch_stream<256, 2>(a, s);
         }
         return rows == 1 ? launch_rows<__nv_bfloat16, 1>(a, s) : rows == 2 ? launch_rows<__nv_bfloat16, 2>(a, s) : launch_rows<__nv_bfloat16, 4>(a, s);
     }

@@ -327,3 +327,26 @@ def test_wide_heads(vd, size):
     again = vd.op_cross_attention(q, k, v, lens, scale=scale)
     torch.cuda.synchronize()
     assert torch.equal(first.view(torch.int16), again.view(torch.int16))
+
+
+@pytest.mark.parametrize("size", [(3, 1, 3000, 8, 4, 256), (2, 4, 5000, 4, 2, 192), (5, 2, 900, 16, 2, 256), (40, 1, 700, 8, 8, 256), (4, 1, 2000, 2, 2, 136), (3, 8, 70, 4, 2, 200)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_wide_heads_of_few_rows(vd, size):
+    """One to sixteen rows of a key head beyond 128 channels: lengths from none to all, NaN behind each, growing scores, the same bits again."""
+    import torch
+    b, _, tk = size[:3]
+    q, k, v = make("bf16", *size, seed=15)
+    k *= 1 + 8 * torch.arange(tk, device="cuda", dtype=k.dtype)[None, :, None, None] / tk
+    lens = torch.tensor([tk - (i * tk) // (b - 1) for i in range(b)], dtype=torch.int32, device="cuda")
+    behind = torch.arange(tk, device="cuda")[None, :, None, None] >= lens[:, None, None, None]
+    scale = q.shape[3] ** -0.5
+    want = block_ref.attention(q, k.masked_fill(behind, 0), v.masked_fill(behind, 0), lens, scale)
+    k.masked_fill_(behind, math.nan)
+    v.masked_fill_(behind, math.nan)
+    first = vd.op_cross_attention(q, k, v, lens, scale=scale)
+    torch.cuda.synchronize()
+    block_ref.check(first, *want)
+    assert (first[lens == 0] == 0).all()
+    again = vd.op_cross_attention(q, k, v, lens, scale=scale)
+    torch.cuda.synchronize()
+    assert torch.equal(first.view(torch.int16), again.view(torch.int16))
