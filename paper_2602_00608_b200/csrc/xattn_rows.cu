@@ -446,8 +446,10 @@ cudaError_t launch_xattn_rows(const XAttnArgs& a, cudaStream_t s) {
         // One row: few heads with long contexts want the ring's bytes in flight, many heads have them anyway and short contexts end
         // sooner without it (us, lanes / ring: 16 heads x 16000 keys of 64 23.5 / 16.6, 4 x 8000 of 128, 4 rows 33.7 / 12.5; 256 x 2000 43.1 / 45.4,
         // 32 x 100 4.8 / 6.5).  Two to four rows: 256 x 2000, two rows 48.0 / 45.8, 32 x 16384, four rows 103 / 47.
-        // Heads of 256: 32 x 16384, one row 82 / 86, four 150 / 87, sixteen of 8000 keys 259 / 58; 4 x 500, two rows 8.3 / 10.6.
-        if ((rows > 1 || (a.D <= 128 && a.Tk > 1024 && (int64_t)a.B * a.Hkv < 148)) && kv_maps_supported(a, 256)) {
+        // Heads of 256: 32 x 16384, one row 82 / 86, four 150 / 87, sixteen of 8000 keys 259 / 58.  Short contexts: 32 x 1000 of 128,
+        // two rows 8.5 / 10.5, x 2000 11.1 / 10.9; 256 x 50, four rows 8.6 / 14.5, x 200 17.1 / 14.6.
+        const bool ring = rows > 4 || a.Tk > (rows > 2 ? 128 : 1024);
+        if ((rows > 1 ? ring : ring && a.D <= 128 && (int64_t)a.B * a.Hkv < 148) && kv_maps_supported(a, 256)) {
             if (a.D <= 64) return rows <= 8 ? launch_stream<64, 1>(a, s) : launch_stream<64, 2>(a, s);
             if (a.D <= 128) return rows <= 8 ? launch_stream<128, 1>(a, s) : launch_stream<128, 2>(a, s);
             return rows <= 8 ? launch_stream<256, 1>(a, s) : launch_stream<256, 2>(a, s);

@@ -350,3 +350,11 @@ def test_wide_heads_of_few_rows(vd, size):
     again = vd.op_cross_attention(q, k, v, lens, scale=scale)
     torch.cuda.synchronize()
     assert torch.equal(first.view(torch.int16), again.view(torch.int16))
+
+
+@pytest.mark.parametrize("size", [(4, 1, 77, 16, 2, 64), (6, 2, 128, 8, 1, 64), (40, 1, 500, 64, 4, 128), (3, 3, 100, 4, 2, 64), (5, 2, 90, 2, 2, 72), (5, 1, 1024, 4, 2, 64), (5, 4, 128, 2, 2, 128),
+                                  (5, 4, 129, 2, 2, 128), (5, 1, 1025, 4, 2, 128), (3, 1, 513, 9, 1, 64), (3, 8, 129, 2, 2, 256), (75, 3, 700, 8, 2, 128)], ids=lambda s: "x".join(map(str, s)))
+def test_few_rows_on_either_side_of_the_rules(vd, size):
+    """Two to sixteen rows of a key head with contexts around the lengths at which another kernel takes them."""
+    b, _, tk = size[:3]
+    run(vd, *make("bf16", *size, seed=16), lens=[(5 * i + tk) % (tk + 1) if i % 3 else tk - i // 3 for i in range(b)])
