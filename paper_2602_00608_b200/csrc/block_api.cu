@@ -69,13 +69,16 @@ vd_status vd_op_cross_attention(const vd_xattn_desc* d, const void* q, const voi
                 {d->q_batch, d->q_token, d->q_head}, {d->k_batch, d->k_token, d->k_head}, {d->v_batch, d->v_token, d->v_head},
                 {d->o_batch, d->o_token, d->o_head}, d->scale};
     const int64_t rows = (int64_t)d->q_len * (d->heads / d->kv_heads);       // of a key head
+    // fp32, four rows of a key head at a time, against tiles of 128 rows (64 beyond 80 channels), us: 256 x 1500 of 64, 32 rows 201 / 342, 64 rows 384 / 344; of 80,
+    // 32 rows 359 / 436; of 128, 16 rows 210 / 342, 32 rows 361 / 342; 256 x 50 of 128, 16 rows 18.7 / 20.8, 24 rows 25.2 / 20.9.
+    const int few = d->dtype == VD_BF16 ? 16 : d->head_dim <= 80 ? 32 : 16;
     // A few rows with a short context: streaming has not begun when it ends, and tiles mostly empty cost less (us, rows kernel / tiles: 1024 x 50, 8 rows of
     // 64 29 / 15; 32 x 100, 8 rows of 128 8.5 / 8.5; 32 x 300, 16 rows of 128 14.7 / 10.6; 256 x 300, 8 rows of 64 12.6 / 14.7; 32 x 1000, 16 rows of 64
     // 10.6 / 16.5).  With 9 to 16 rows of more than 64 channels in every SM the products bound the rows kernel (256 x 1000 of 128 38.6 / 35.1, of
     // 256 72 / 53; x 4000 of 128 90 / 102).
     const bool tiles = d->dtype == VD_BF16 && rows > 4 && (a.Tk <= 128 || (rows > 8 && (a.Tk <= 512 || (a.D > 64 && a.Tk <= 2048 && (int64_t)a.B * a.Hkv >= 148))));
     cudaError_t e;
-    if (d->impl == VD_XATTN_AUTO && rows <= (d->dtype == VD_BF16 ? 16 : 4) && xattn_rows_supported(a) && !(tiles && xattn_tc_supported(a))) e = launch_xattn_rows(a, (cudaStream_t)cuda_stream);
+    if (d->impl == VD_XATTN_AUTO && rows <= few && xattn_rows_supported(a) && !(tiles && xattn_tc_supported(a))) e = launch_xattn_rows(a, (cudaStream_t)cuda_stream);
     else if (d->impl == VD_XATTN_AUTO && d->dtype == VD_BF16 && xattn_tc_supported(a)) e = launch_xattn_tc(a, (cudaStream_t)cuda_stream);
     else if (d->impl == VD_XATTN_AUTO) e = launch_xattn_f32(a, (cudaStream_t)cuda_stream);
     else e = launch_xattn_plain(a, (cudaStream_t)cuda_stream);

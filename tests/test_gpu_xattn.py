@@ -358,3 +358,11 @@ def test_few_rows_on_either_side_of_the_rules(vd, size):
     """Two to sixteen rows of a key head with contexts around the lengths at which another kernel takes them."""
     b, _, tk = size[:3]
     run(vd, *make("bf16", *size, seed=16), lens=[(5 * i + tk) % (tk + 1) if i % 3 else tk - i // 3 for i in range(b)])
+
+
+@pytest.mark.parametrize("size", [(3, 5, 300, 4, 4, 64), (2, 8, 500, 8, 2, 80), (2, 11, 130, 6, 2, 64), (3, 2, 700, 16, 2, 128), (2, 17, 90, 1, 1, 96), (2, 1, 1000, 31, 1, 40), (70, 3, 40, 10, 5, 64),
+                                  (3, 4, 600, 8, 2, 256)], ids=lambda s: "x".join(map(str, s)))
+def test_few_rows_in_single_precision(vd, size):
+    """Five to 33 rows of a key head, in groups of four: a length for each sequence, none and all among them."""
+    b, _, tk = size[:3]
+    run(vd, *make("f32", *size, seed=17), lens=[(5 * i + tk) % (tk + 1) if i % 3 else tk - i // 3 for i in range(b)])
