@@ -87,22 +87,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {       // NaN 
     return y;
 }
 __device__ __forceinline__ void unpack2(unsigned long long v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
-// 2^x for a pair of x <= 8 on the FMA pipes: x = n + f, |f| <= 1/2, a polynomial of degree 4 for 2^f (coefficients fitted here to the
-// least largest relative error, 2^-18.5), n added to the exponent.  Below 2^-126 the result stays there.
-__device__ __forceinline__ void ex2_poly2(float& x, float& y) {
-    const unsigned long long v = pack2(fmaxf(x, -126.f), fmaxf(y, -126.f));
-    const unsigned long long t = add2(v, pack2(12582912.f, 12582912.f));             // 1.5 * 2^23: the sum's low bits are n
-    const unsigned long long f = fmaf2(add2(t, pack2(-12582912.f, -12582912.f)), pack2(-1.f, -1.f), v);
-    unsigned long long p = fmaf2(f, pack2(0.009570102f, 0.009570102f), pack2(0.055917859f, 0.055917859f));
-    p = fmaf2(p, f, pack2(0.24024744f, 0.24024744f));
-    p = fmaf2(p, f, pack2(0.69312179f, 0.69312179f));
-    p = fmaf2(p, f, pack2(0.99999928f, 0.99999928f));
-    float a, b, tx, ty;
-    unpack2(p, a, b);
-    unpack2(t, tx, ty);
-    x = __uint_as_float(__float_as_uint(a) + (__float_as_uint(tx) << 23));
-    y = __uint_as_float(__float_as_uint(b) + (__float_as_uint(ty) << 23));
-}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
@@ -127,8 +111,8 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
-// N = 32 or 16 scores into as many numbers of P: 2^(score * scale - reference), their sums, bf16; every POLY-th pair on the FMA pipes
-template <int POLY, int N = 32>
+// N = 32 or 16 scores into as many numbers of P: 2^(score * scale - reference), their sums, bf16
+template <int N = 32>
 __device__ __forceinline__ void exp_chunk(const uint32_t (&r)[32], uint32_t t_p, unsigned long long sc, unsigned long long mr,
                                           unsigned long long& sum, unsigned long long& sum_b) {
     uint32_t pk[16];
@@ -136,12 +120,8 @@ __device__ __forceinline__ void exp_chunk(const uint32_t (&r)[32], uint32_t t_p,
     for (int q = 0; q < N; q += 2) {
         float e0, e1;
         unpack2(fmaf2(pack2(__uint_as_float(r[q]), __uint_as_float(r[q + 1])), sc, mr), e0, e1);
-        if (POLY && (q / 2) % (POLY ? POLY : 1) == POLY - 1) {
-            ex2_poly2(e0, e1);
-        } else {
-            e0 = ex2(e0);
-            e1 = ex2(e1);
-        }
+        e0 = ex2(e0);
+        e1 = ex2(e1);
         if (q & 2) sum_b = add2(sum_b, pack2(e0, e1));
         else sum = add2(sum, pack2(e0, e1));
         pk[q >> 1] = pack_bf16(e0, e1);
@@ -243,9 +223,9 @@ template <int DP> struct Tile {
         move_reference(t0 * scale_log2, 0u);
         const unsigned long long sc = pack2(scale_log2, scale_log2);
         unsigned long long mr = minus_ref();
-        exp_chunk<0>(a, t_p, sc, mr, sum, sum_b);
+        exp_chunk(a, t_p, sc, mr, sum, sum_b);
         tmem_ld32(t_s + 96u, a);
-        exp_chunk<0>(b, t_p + 16u, sc, mr, sum, sum_b);
+        exp_chunk(b, t_p + 16u, sc, mr, sum, sum_b);
         tmem_ld_wait();
         if (s_free) hand_over(s_free, lane);
         const float t1 = max_of(a, max_of(c, t0));
@@ -253,15 +233,12 @@ template <int DP> struct Tile {
         tmem_st_wait();
         hand_over(first_half, lane);
         mr = minus_ref();
-        exp_chunk<0>(c, t_p + 32u, sc, mr, sum, sum_b);
-        exp_chunk<0>(a, t_p + 48u, sc, mr, sum, sum_b);
+        exp_chunk(c, t_p + 32u, sc, mr, sum, sum_b);
+        exp_chunk(a, t_p + 48u, sc, mr, sum, sum_b);
         return t1;
     }
     // The same where only the first `valid` <= 96 keys count: the others leave before the maximum, 16 keys are the least that is worked on.
-    // A quarter of the exponentials on the FMA pipes (five instructions for one): this is a context's last tile, which little overlaps (8 x 1350 x 1350,
-    // 30 heads of 64 194.8 -> 192; in full() a 16th made no difference, an 8th was slower).
     __device__ __forceinline__ float most(int valid, uint64_t* first_half) {
-        constexpr int POLY = 4;
         uint32_t a[32], b[32], c[32];
         tmem_ld32(t_s, a);
         tmem_ld32(t_s + 32u, b);
@@ -280,14 +257,14 @@ template <int DP> struct Tile {
         wait_pv();
         move_reference(top * scale_log2, 0u);
         const unsigned long long sc = pack2(scale_log2, scale_log2), mr = minus_ref();
-        if (valid > 16) exp_chunk<POLY>(a, t_p, sc, mr, sum, sum_b);
-        else exp_chunk<POLY, 16>(a, t_p, sc, mr, sum, sum_b);
-        if (valid > 48) exp_chunk<POLY>(b, t_p + 16u, sc, mr, sum, sum_b);
-        else if (valid > 32) exp_chunk<POLY, 16>(b, t_p + 16u, sc, mr, sum, sum_b);
+        if (valid > 16) exp_chunk(a, t_p, sc, mr, sum, sum_b);
+        else exp_chunk<16>(a, t_p, sc, mr, sum, sum_b);
+        if (valid > 48) exp_chunk(b, t_p + 16u, sc, mr, sum, sum_b);
+        else if (valid > 32) exp_chunk<16>(b, t_p + 16u, sc, mr, sum, sum_b);
         tmem_st_wait();
         hand_over(first_half, lane);
-        if (valid > 80) exp_chunk<POLY>(c, t_p + 32u, sc, mr, sum, sum_b);
-        else if (valid > 64) exp_chunk<POLY, 16>(c, t_p + 32u, sc, mr, sum, sum_b);
+        if (valid > 80) exp_chunk(c, t_p + 32u, sc, mr, sum, sum_b);
+        else if (valid > 64) exp_chunk<16>(c, t_p + 32u, sc, mr, sum, sum_b);
         return top;
     }
     // The same for any number of them, 32 at a time.  (The code of full() with masks spills.)
@@ -309,7 +286,7 @@ template <int DP> struct Tile {
             tmem_ld32(t_s + (uint32_t)c, r);
             tmem_ld_wait();
             if (valid - c < 32) mask(r, valid - c);
-            exp_chunk<0>(r, t_p + (uint32_t)(c >> 1), sc, mr, sum, sum_b);
+            exp_chunk(r, t_p + (uint32_t)(c >> 1), sc, mr, sum, sum_b);
         }
         tmem_st_wait();
         hand_over(first_half, lane);
@@ -336,10 +313,10 @@ template <int DP> struct Tile {
                 tmem_ld_wait();
                 if (valid - c > 16) {
                     if (valid - c < 32) mask(r, valid - c);
-                    exp_chunk<0>(r, t_p + (uint32_t)(c >> 1), sc, mr, sum, sum_b);
+                    exp_chunk(r, t_p + (uint32_t)(c >> 1), sc, mr, sum, sum_b);
                 } else {
                     mask<16>(r, valid - c);
-                    exp_chunk<0, 16>(r, t_p + (uint32_t)(c >> 1), sc, mr, sum, sum_b);
+                    exp_chunk<16>(r, t_p + (uint32_t)(c >> 1), sc, mr, sum, sum_b);
                 }
             }
         return top;

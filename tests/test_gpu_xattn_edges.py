@@ -1,0 +1,63 @@
+"""Attention to states of another length at the edges of its numbers: rows whose every score is minus infinity, weights that
+underflow, one key, scores far from zero."""
+import math
+
+import pytest
+
+from tests import block_ref
+
+pytestmark = pytest.mark.gpu
+
+WIDTHS = [64, 72, 128, 256]
+CONTEXTS = [1, 17, 20, 77, 96, 100, 128, 150, 224, 256, 333]         # last tiles of every kind, alone and behind whole ones
+
+
+@pytest.fixture(scope="module")
+def vd():
+    from paper_2602_00608_b200 import binding
+    return binding
+
+
+def make(dtype, b, tq, tk, h, hkv, d, seed):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(7000 + seed)
+    dt = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    return tuple(torch.randn(s, generator=g, device="cuda").to(dt) for s in ((b, tq, h, d), (b, tk, hkv, d), (b, tk, hkv, d)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tq", [1, 3, 8, 40])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_scores_of_minus_infinity(vd, dtype, tq, d):
+    """A row all of whose scores are minus infinity is 0 / 0, as in the definition, whatever the number of keys; such scores beside finite ones
+    weigh nothing."""
+    import torch
+    for tk in CONTEXTS:
+        q, k, v = make(dtype, 2, tq, tk, 2, 2, d, seed=1)
+        q[..., 0] = 1
+        k[0, :, :, 0] = -math.inf
+        few = min(tk, 3)
+        k[1, few:, :, 0] = -math.inf
+        o = vd.op_cross_attention(q, k, v, scale=0.125)
+        torch.cuda.synchronize()
+        assert torch.isnan(o[0]).all(), f"{tk} keys: {float(torch.isnan(o[0]).float().mean()):.2f} NaN"
+        block_ref.check(o[1:], *block_ref.attention(q[1:], k[1:, :few], v[1:, :few], None, 0.125))
+
+
+@pytest.mark.parametrize("tq", [1, 3, 8, 40])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_weights_that_underflow_are_zero(vd, tq, d):
+    """The first key's score is above the others' by 1024 (1477 in units of log 2: 2^-1477 is 0 in fp32), so the row is that key's value, however
+    large the others' are (1e36 each: no sum of 100 of them overflows).  The output is v times a sum of ones and zeros over itself, rounded: exact, but
+    for the probability's and the output's half steps."""
+    import torch
+    for tk in (17, 20, 77, 96, 100, 128):
+        q, k, v = make("bf16", 1, tq, tk, 2, 2, d, seed=2)
+        q.zero_()
+        k.zero_()
+        q[..., 0], k[:, 0, :, 0], v[:, 1:] = 64.0, 64.0, 1e36
+        o = vd.op_cross_attention(q, k, v, scale=0.25)
+        torch.cuda.synchronize()
+        want = v[:, :1].double().expand(o.shape)
+        off = ((o.double() - want).abs() - 2.01 * block_ref.BF16 * want.abs()).max()
+        assert off <= 0, f"{tk} keys: off by {float((o.double() - want).abs().max()):.3g}"
