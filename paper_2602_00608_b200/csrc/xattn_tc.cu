@@ -160,16 +160,17 @@ template <int DP> struct Tile {
     unsigned long long sum, sum_b;       // of even and odd pairs of keys
     bool ok = true;
 
-    // The reference is an integer that the exponentials are relative to: it stays unless a score exceeds it by more than the threshold, and
-    // moves by a power of two, so that what has been summed (O, the sums, P as far as it is written) is rescaled without rounding.
+    // What the exponentials are relative to: at first the maximum itself, whose P is then 1 and is not rounded (a row that one key has, or all
+    // but has, is that key's value).  It stays unless a score exceeds it by more than the threshold, and moves by a whole number, so
+    // that what has been summed (O, the sums, P as far as it is written) is rescaled by a power of two, without rounding.
     __device__ __forceinline__ void move_reference(float top, uint32_t p_cols) {
         const bool grow = top > m_ref + RESCALE_THRESHOLD;
         if (!__any_sync(0xffffffffu, grow)) return;
         float factor = 1.f;
         if (grow) {
-            const float to = ceilf(top), by = to - m_ref;    // (infinite at the first tile)
+            const float by = ceilf(top - m_ref);             // (infinite at the first tile)
             factor = by < 127.f ? __int_as_float((127 - (int)by) << 23) : 0.f;
-            m_ref = to;
+            m_ref = by < 127.f ? m_ref + by : top;
         }
         sum = fmaf2(sum, pack2(factor, factor), 0ull);
         sum_b = fmaf2(sum_b, pack2(factor, factor), 0ull);

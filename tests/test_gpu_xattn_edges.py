@@ -61,3 +61,20 @@ def test_weights_that_underflow_are_zero(vd, tq, d):
         want = v[:, :1].double().expand(o.shape)
         off = ((o.double() - want).abs() - 2.01 * block_ref.BF16 * want.abs()).max()
         assert off <= 0, f"{tk} keys: off by {float((o.double() - want).abs().max()):.3g}"
+
+
+@pytest.mark.parametrize("tq", [1, 3, 8, 40, 300])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_one_key_is_its_value(vd, tq, d):
+    """softmax of one score is 1: the output is v, bit for bit.  The same where one key's score is above all others by 200 in units of log 2 (their
+    weights are 2^-200), in the first tile of keys or in one behind it."""
+    import torch
+    for tk in CONTEXTS:
+        q, k, v = make("bf16", 2, tq, tk, 4, 2, d, seed=3)
+        o = vd.op_cross_attention(q, k, v, torch.ones(2, dtype=torch.int32, device="cuda"))
+        assert torch.equal(o, v[:, :1].repeat_interleave(2, 2).expand_as(o)), f"one of {tk} keys"
+        for at in {0, tk // 3, tk // 2, tk - 1}:
+            q[..., 0], k[..., 0] = 16.0, 0.0
+            k[:, at, :, 0] = 512.0 + 16.0 * d
+            o = vd.op_cross_attention(q, k, v, scale=0.25)
+            assert torch.equal(o, v[:, at:at + 1].repeat_interleave(2, 2).expand_as(o)), f"key {at} of {tk}"
