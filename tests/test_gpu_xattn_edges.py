@@ -78,3 +78,32 @@ def test_one_key_is_its_value(vd, tq, d):
             k[:, at, :, 0] = 512.0 + 16.0 * d
             o = vd.op_cross_attention(q, k, v, scale=0.25)
             assert torch.equal(o, v[:, at:at + 1].repeat_interleave(2, 2).expand_as(o)), f"key {at} of {tk}"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tq", [1, 3, 8, 40, 300])
+@pytest.mark.parametrize("d", WIDTHS)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_far_from_zero(vd, dtype, tq, d, sign):
+    """Scores of up to 2^107, above zero and below, whose size varies within a row: two keys share the largest, and the next is lower by
+    thousands, so the row is the mean of the two values (weights 1 + 1; off by the half steps of the probabilities, which are alike, and of the output).
+    Each score is one product of numbers of at most eight bits, exact in fp32; the scale is no power of two."""
+    import torch
+    half = block_ref.half_step(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    g = torch.Generator(device="cuda").manual_seed(7004)
+    for tk in (77, 90, 150, 333, 3000):
+        for e in (8, 16, 21, 24, 27, 30, 33, 40, 60, 98):
+            q, k, v = make(dtype, 1, tq, tk, 2, 1, d, seed=4)
+            q.zero_()
+            k.zero_()
+            q[..., 0] = 2.0 ** (e // 2)
+            odd = (2 * torch.randint(64, 128, (tk,), generator=g, device="cuda") + 1).float()                    # 129 to 255
+            less = 2.0 ** -torch.randint(1, e - 6, (tk,), generator=g, device="cuda").float() if sign > 0 else 1.0
+            k[0, :, 0, 0] = sign * odd * less * 2.0 ** (e - e // 2)
+            i, j = sorted(torch.randperm(tk, generator=g, device="cuda")[:2].tolist())
+            k[0, [i, j], 0, 0] = sign * (251.0 if sign > 0 else 67.0) * 2.0 ** (e - e // 2)
+            o = vd.op_cross_attention(q, k, v, scale=72.0 ** -0.5)
+            torch.cuda.synchronize()
+            one, two = v[0, i, 0].double(), v[0, j, 0].double()
+            off = (o.double() - (one + two) / 2).abs() - 2.01 * half * (one.abs() + two.abs()) / 2
+            assert (off <= 0).all(), f"{tk} keys, 2^{e}, the largest at {i} and {j}: {int((~(off <= 0)).sum())} values"
