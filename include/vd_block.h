@@ -51,6 +51,11 @@ typedef struct {
 VD_API vd_status vd_op_cross_attention(const vd_xattn_desc* d, const void* q, const void* k, const void* v,
                                        const int32_t* kv_lens, void* o, void* cuda_stream);
 
+/* Test hook: how a bf16 call of the tensor-core kernel (aligned tensors) is shared out on the current device: of its `items` (up to 256
+ * rows of a key head) the first `whole` are a thread block's each, the others a cluster's of `splits` blocks, which divide the keys.
+ * VD_ERR_UNSUPPORTED where another kernel takes the call.  Launches nothing. */
+VD_API vd_status vd_debug_xattn_division(const vd_xattn_desc* d, int32_t* splits, int64_t* items, int64_t* whole);
+
 /* ------------------------------------------------------------------------------------------
  * Rotary positions.  The first rotary_dim channels of a head are rotary_dim / 2 pairs; pair i of a token turns by
  * position[axis of i] * freqs[i]:   (a, b) -> amplitude * (a cos - b sin, a sin + b cos);   the other channels are copied.

@@ -42,22 +42,46 @@ bool not_negative(const int64_t* s, int n) {
     return true;
 }
 
+const char* xattn_error(const vd_xattn_desc* d) {
+    if (!d) return "NULL descriptor";
+    if (d->struct_size != sizeof(vd_xattn_desc)) return "vd_xattn_desc: struct_size mismatch";
+    if (!is_dtype(d->dtype)) return "bad dtype";
+    if (d->batch < 0 || d->q_len < 0 || d->kv_len < 0 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0 ||
+        d->head_dim < 1 || d->head_dim > 256 || d->kv_len > 1 << 25 || !fits(d->batch, d->heads, d->q_len) ||
+        (int64_t)d->batch * d->heads * d->q_len > 1 << 30)
+        return "bad attention sizes";
+    if (d->impl < VD_XATTN_AUTO || d->impl > VD_XATTN_PLAIN) return "bad impl";
+    if (!(d->scale > 0.f) || isinf(d->scale)) return "scale must be positive and finite";
+    if (!not_negative(&d->q_batch, 12)) return "negative stride";
+    return nullptr;
+}
+XAttnArgs xattn_args(const vd_xattn_desc* d, const void* q, const void* k, const void* v, const int32_t* kv_lens, void* o) {
+    return {q, k, v, o, kv_lens, d->dtype, d->batch, d->q_len, d->kv_len, d->heads, d->kv_heads, d->head_dim,
+            {d->q_batch, d->q_token, d->q_head}, {d->k_batch, d->k_token, d->k_head}, {d->v_batch, d->v_token, d->v_head},
+            {d->o_batch, d->o_token, d->o_head}, d->scale};
+}
+// the kernel that takes a call
+auto kernel_of(const XAttnArgs& a) -> cudaError_t (*)(const XAttnArgs&, cudaStream_t) {
+    const int64_t rows = (int64_t)a.Tq * (a.H / a.Hkv);       // of a key head
+    // fp32, four rows of a key head at a time, against tiles of 128 rows (64 beyond 80 channels), us: 256 x 1500 of 64, 32 rows 201 / 342, 64 rows 384 / 344; of 80,
+    // 32 rows 359 / 436; of 128, 16 rows 210 / 342, 32 rows 361 / 342; 256 x 50 of 128, 16 rows 18.7 / 20.8, 24 rows 25.2 / 20.9.
+    const int few = a.dtype == VD_BF16 ? 16 : a.D <= 80 ? 32 : 16;
+    // A few rows with a short context: streaming has not begun when it ends, and tiles mostly empty cost less (us, rows kernel / tiles: 1024 x 50, 8 rows of
+    // 64 29 / 15; 32 x 100, 8 rows of 128 8.5 / 8.5; 32 x 300, 16 rows of 128 14.7 / 10.6; 256 x 300, 8 rows of 64 12.6 / 14.7; 32 x 1000, 16 rows of 64
+    // 10.6 / 16.5).  With 9 to 16 rows of more than 64 channels in every SM the products bound the rows kernel (256 x 1000 of 128 38.6 / 35.1, of
+    // 256 72 / 53; x 4000 of 128 90 / 102).
+    const bool tiles = a.dtype == VD_BF16 && rows > 4 && (a.Tk <= 128 || (rows > 8 && (a.Tk <= 512 || (a.D > 64 && a.Tk <= 2048 && (int64_t)a.B * a.Hkv >= 148))));
+    if (rows <= few && xattn_rows_supported(a) && !(tiles && xattn_tc_supported(a))) return launch_xattn_rows;
+    return a.dtype == VD_BF16 && xattn_tc_supported(a) ? launch_xattn_tc : launch_xattn_f32;
+}
+
 }  // namespace
 
 extern "C" {
 
 vd_status vd_op_cross_attention(const vd_xattn_desc* d, const void* q, const void* k, const void* v, const int32_t* kv_lens, void* o,
                                 void* cuda_stream) {
-    if (!d) return refuse(VD_ERR_INVALID_ARG, "NULL descriptor");
-    if (d->struct_size != sizeof(vd_xattn_desc)) return refuse(VD_ERR_INVALID_ARG, "vd_xattn_desc: struct_size mismatch");
-    if (!is_dtype(d->dtype)) return refuse(VD_ERR_INVALID_ARG, "bad dtype");
-    if (d->batch < 0 || d->q_len < 0 || d->kv_len < 0 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0 ||
-        d->head_dim < 1 || d->head_dim > 256 || d->kv_len > 1 << 25 || !fits(d->batch, d->heads, d->q_len) ||
-        (int64_t)d->batch * d->heads * d->q_len > 1 << 30)
-        return refuse(VD_ERR_INVALID_ARG, "bad attention sizes");
-    if (d->impl < VD_XATTN_AUTO || d->impl > VD_XATTN_PLAIN) return refuse(VD_ERR_INVALID_ARG, "bad impl");
-    if (!(d->scale > 0.f) || isinf(d->scale)) return refuse(VD_ERR_INVALID_ARG, "scale must be positive and finite");
-    if (!not_negative(&d->q_batch, 12)) return refuse(VD_ERR_INVALID_ARG, "negative stride");
+    if (const char* e = xattn_error(d)) return refuse(VD_ERR_INVALID_ARG, e);
     if (d->batch == 0 || d->q_len == 0) return VD_OK;
     if (!distinct(d->batch, d->o_batch, d->q_len, d->o_token, d->heads, d->o_head, d->head_dim))
         return refuse(VD_ERR_INVALID_ARG, "elements of the output overlap");
@@ -65,24 +89,25 @@ vd_status vd_op_cross_attention(const vd_xattn_desc* d, const void* q, const voi
     if (!aligned_to(q, d->dtype) || !aligned_to(k, d->dtype) || !aligned_to(v, d->dtype) || !aligned_to(o, d->dtype) || ((uintptr_t)kv_lens & 3))
         return refuse(VD_ERR_INVALID_ARG, "misaligned pointer");
     if (o == q || o == k || o == v) return refuse(VD_ERR_INVALID_ARG, "o is an input");
-    XAttnArgs a{q, k, v, o, kv_lens, d->dtype, d->batch, d->q_len, d->kv_len, d->heads, d->kv_heads, d->head_dim,
-                {d->q_batch, d->q_token, d->q_head}, {d->k_batch, d->k_token, d->k_head}, {d->v_batch, d->v_token, d->v_head},
-                {d->o_batch, d->o_token, d->o_head}, d->scale};
-    const int64_t rows = (int64_t)d->q_len * (d->heads / d->kv_heads);       // of a key head
-    // fp32, four rows of a key head at a time, against tiles of 128 rows (64 beyond 80 channels), us: 256 x 1500 of 64, 32 rows 201 / 342, 64 rows 384 / 344; of 80,
-    // 32 rows 359 / 436; of 128, 16 rows 210 / 342, 32 rows 361 / 342; 256 x 50 of 128, 16 rows 18.7 / 20.8, 24 rows 25.2 / 20.9.
-    const int few = d->dtype == VD_BF16 ? 16 : d->head_dim <= 80 ? 32 : 16;
-    // A few rows with a short context: streaming has not begun when it ends, and tiles mostly empty cost less (us, rows kernel / tiles: 1024 x 50, 8 rows of
-    // 64 29 / 15; 32 x 100, 8 rows of 128 8.5 / 8.5; 32 x 300, 16 rows of 128 14.7 / 10.6; 256 x 300, 8 rows of 64 12.6 / 14.7; 32 x 1000, 16 rows of 64
-    // 10.6 / 16.5).  With 9 to 16 rows of more than 64 channels in every SM the products bound the rows kernel (256 x 1000 of 128 38.6 / 35.1, of
-    // 256 72 / 53; x 4000 of 128 90 / 102).
-    const bool tiles = d->dtype == VD_BF16 && rows > 4 && (a.Tk <= 128 || (rows > 8 && (a.Tk <= 512 || (a.D > 64 && a.Tk <= 2048 && (int64_t)a.B * a.Hkv >= 148))));
-    cudaError_t e;
-    if (d->impl == VD_XATTN_AUTO && rows <= few && xattn_rows_supported(a) && !(tiles && xattn_tc_supported(a))) e = launch_xattn_rows(a, (cudaStream_t)cuda_stream);
-    else if (d->impl == VD_XATTN_AUTO && d->dtype == VD_BF16 && xattn_tc_supported(a)) e = launch_xattn_tc(a, (cudaStream_t)cuda_stream);
-    else if (d->impl == VD_XATTN_AUTO) e = launch_xattn_f32(a, (cudaStream_t)cuda_stream);
-    else e = launch_xattn_plain(a, (cudaStream_t)cuda_stream);
-    return done(e, "vd_op_cross_attention");
+    const XAttnArgs a = xattn_args(d, q, k, v, kv_lens, o);
+    const auto launch = d->impl == VD_XATTN_PLAIN ? launch_xattn_plain : kernel_of(a);
+    return done(launch(a, (cudaStream_t)cuda_stream), "vd_op_cross_attention");
+}
+
+vd_status vd_debug_xattn_division(const vd_xattn_desc* d, int32_t* splits, int64_t* items, int64_t* whole) {
+    if (const char* e = xattn_error(d)) return refuse(VD_ERR_INVALID_ARG, e);
+    if (!splits || !items || !whole) return refuse(VD_ERR_INVALID_ARG, "NULL pointer");
+    const uintptr_t at = 4096;
+    const XAttnArgs a = xattn_args(d, (void*)at, (void*)at, (void*)at, nullptr, (void*)at);
+    if (d->batch == 0 || d->q_len == 0 || d->impl != VD_XATTN_AUTO || kernel_of(a) != launch_xattn_tc)
+        return refuse(VD_ERR_UNSUPPORTED, "another kernel takes this call");
+    XAttnDivision div;
+    const cudaError_t e = xattn_tc_division(a, &div);
+    if (e != cudaSuccess) return done(e, "vd_debug_xattn_division");
+    *splits = div.splits;
+    *items = div.items;
+    *whole = div.whole;
+    return VD_OK;
 }
 
 static const char* rotary_axes_error(int rotary_dim, int axes, const int32_t* pairs) {

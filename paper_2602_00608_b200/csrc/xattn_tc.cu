@@ -874,55 +874,45 @@ bool encode_rows(CUtensorMap* tm, const XAttnArgs& a, const void* p, const Strid
 
 // How the items are shared out: as many rounds of whole ones as fill every CTA, and the rest (all, where there are few) divided by keys within
 // clusters.  The fewest tiles in a row, counting what an item (a meeting) costs besides its tiles.
-struct Division { int splits; uint32_t whole, grid; };
-template <int DP> Division divide(uint32_t items, int Tk, int sms) {
+template <int DP> XAttnDivision divide(uint32_t items, int Tk, int sms) {
     const int64_t tiles = (Tk + KEYS - 1) / KEYS;
-    Division best{1, items, std::min(items, (uint32_t)sms)};
-    double cost = (double)((items + best.grid - 1) / best.grid) * (double)(tiles + 1);
-    for (int n = 2; n <= MAX_SPLITS && n <= tiles; ++n) {
-        const int held = xa::clusters_held<xattn_tc_kernel<DP, ALL>>(NUM_THREADS, Cfg<DP>::SMEM, n);      // (REST has the same shape)
-        if (held < 1) continue;
-        const uint32_t ctas = (uint32_t)(held * n), whole = items / ctas * ctas, left = items - whole;
-        if (left == 0) continue;
-        const double c = (double)(whole / ctas) * (double)(tiles + 1) +
-                         (double)((left + held - 1) / held) * ((double)((tiles + n - 1) / n) + (whole ? MEET_REST : MEET_ALL));
-        if (c < cost) { cost = c; best = {n, whole, whole ? ctas : std::min(left, (uint32_t)held) * (uint32_t)n}; }
+    XAttnDivision best{1, items, items, std::min(items, (uint32_t)sms)};
+    if (DP == 64 && Tk <= KEYS) {
+        best.grid = std::min(items, 2u * (uint32_t)sms);
+        return best;
+    }
+    if constexpr (DP < 256) {                                // (wider heads: not divided)
+        double cost = (double)((items + best.grid - 1) / best.grid) * (double)(tiles + 1);
+        for (int n = 2; n <= MAX_SPLITS && n <= tiles; ++n) {
+            const int held = xa::clusters_held<xattn_tc_kernel<DP, ALL>>(NUM_THREADS, Cfg<DP>::SMEM, n);      // (REST has the same shape)
+            if (held < 1) continue;
+            const uint32_t ctas = (uint32_t)(held * n), whole = items / ctas * ctas, left = items - whole;
+            if (left == 0) continue;
+            const double c = (double)(whole / ctas) * (double)(tiles + 1) +
+                             (double)((left + held - 1) / held) * ((double)((tiles + n - 1) / n) + (whole ? MEET_REST : MEET_ALL));
+            if (c < cost) { cost = c; best = {n, items, whole, whole ? ctas : std::min(left, (uint32_t)held) * (uint32_t)n}; }
+        }
     }
     return best;
 }
 
-template <int DP> cudaError_t launch(Params& p, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& to, int sms, cudaStream_t s) {
-    const auto step = [&](uint32_t grid) {
-        const uint32_t heads = grid / (uint32_t)p.q_items;
-        p.dq = (int)(grid % (uint32_t)p.q_items);
-        p.dh = (int)(heads % (uint32_t)p.Hkv);
-        p.db = (int)(heads / (uint32_t)p.Hkv);
-        return grid;
-    };
-    if constexpr (DP == 256) {
-        constexpr int smem = Cfg<DP>::SMEM;
-        p.splits = 1;
-        p.whole = p.items;
-        const uint32_t grid = step(std::min(p.items, (uint32_t)sms));
-        return cc::launch_clusters<xattn_tc_kernel<DP, NONE>>({grid, NUM_THREADS, smem, smem, 1}, s, p, tq, tk, tv, to);
-    } else {
-        if constexpr (DP == 64)
-            if (p.Tk <= KEYS) {
-                constexpr int short_smem = Cfg<DP, true>::SMEM;
-                p.splits = 1;
-                p.whole = p.items;
-                const uint32_t grid = step(std::min(p.items, 2u * (uint32_t)sms));
-                return cc::launch_clusters<xattn_tc_kernel<DP, SHORT>>({grid, NUM_THREADS, short_smem, short_smem, 1}, s, p, tq, tk, tv, to);
-            }
-        constexpr int smem = Cfg<DP>::SMEM;
-        const Division d = divide<DP>(p.items, p.Tk, sms);
-        p.splits = d.splits;
-        p.whole = d.whole;
-        const uint32_t grid = step(d.grid);
-        if (p.splits > 1 && p.whole) return cc::launch_clusters<xattn_tc_kernel<DP, REST>>({grid, NUM_THREADS, smem, smem, p.splits}, s, p, tq, tk, tv, to);
-        if (p.splits > 1) return cc::launch_clusters<xattn_tc_kernel<DP, ALL>>({grid, NUM_THREADS, smem, smem, p.splits}, s, p, tq, tk, tv, to);
-        return cc::launch_clusters<xattn_tc_kernel<DP, NONE>>({grid, NUM_THREADS, smem, smem, 1}, s, p, tq, tk, tv, to);
+template <int DP, int DIVIDED> cudaError_t launch_as(const XAttnDivision& d, const Params& p, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& to, cudaStream_t s) {
+    constexpr int smem = Cfg<DP, DIVIDED == SHORT>::SMEM;
+    return cc::launch_clusters<xattn_tc_kernel<DP, DIVIDED>>({d.grid, NUM_THREADS, smem, smem, d.splits}, s, p, tq, tk, tv, to);
+}
+template <int DP> cudaError_t launch(const XAttnDivision& d, const Params& p, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& to, cudaStream_t s) {
+    if constexpr (DP < 256) {
+        if (d.splits > 1) return d.whole ? launch_as<DP, REST>(d, p, tq, tk, tv, to, s) : launch_as<DP, ALL>(d, p, tq, tk, tv, to, s);
     }
+    if constexpr (DP == 64) {
+        if (p.Tk <= KEYS) return launch_as<DP, SHORT>(d, p, tq, tk, tv, to, s);
+    }
+    return launch_as<DP, NONE>(d, p, tq, tk, tv, to, s);
+}
+
+int items_of_head(const XAttnArgs& a) {                      // tiles of nt tokens, two to an item (one beyond 128 channels)
+    const int tokens = (a.D > 128 ? 1 : 2) * (ROWS / (a.H / a.Hkv));
+    return (a.Tq + tokens - 1) / tokens;
 }
 
 }  // namespace
@@ -937,27 +927,41 @@ bool xattn_tc_supported(const XAttnArgs& a) {
     return kv_maps_supported(a, 256) && g <= ROWS && rows_ok(a.q, a.sq) && rows_ok(a.o, a.so);
 }
 
+cudaError_t xattn_tc_division(const XAttnArgs& a, XAttnDivision* d) {
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    const uint32_t items = (uint32_t)((int64_t)items_of_head(a) * a.Hkv * a.B);      // (rows are at most 2^30)
+    *d = a.D <= 64 ? divide<64>(items, a.Tk, sms) : a.D <= 128 ? divide<128>(items, a.Tk, sms) : divide<256>(items, a.Tk, sms);
+    return cudaSuccess;
+}
+
 cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s) {
     CUtensorMap tq, tk, tv, to;
     Params p;
     p.o = (__nv_bfloat16*)a.o; p.o_batch = a.so.batch; p.o_token = a.so.token; p.o_head = a.so.head;
     p.lens = a.kv_lens;
     p.Tq = a.Tq; p.Tk = a.Tk; p.B = a.B; p.Hkv = a.Hkv; p.g = a.H / a.Hkv; p.D = a.D; p.nt = ROWS / p.g;
-    const int tokens = (a.D > 128 ? 1 : 2) * p.nt;           // of an item
-    p.q_items = (a.Tq + tokens - 1) / tokens;
-    p.items = (uint32_t)((int64_t)p.q_items * a.Hkv * a.B);          // (rows are at most 2^30)
+    p.q_items = items_of_head(a);
     p.scale_log2 = a.scale * 1.4426950408889634f;
     int exponent;
     p.scale_far = frexpf(p.scale_log2, &exponent) == 0.5f ? p.scale_log2 : ldexpf(1.f, exponent);
     if (!encode_rows(&tq, a, a.q, a.sq, p.nt) || !encode_rows(&to, a, a.o, a.so, p.nt) || !encode_kv(&tk, a, a.k, a.sk, KEYS, &p.kh, &p.kb) ||
         !encode_kv(&tv, a, a.v, a.sv, KEYS, &p.vh, &p.vb))
         return cudaErrorInvalidValue;
-    int dev = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    XAttnDivision d;
+    const cudaError_t e = xattn_tc_division(a, &d);
     if (e != cudaSuccess) return e;
-    if (a.D <= 64) return launch<64>(p, tq, tk, tv, to, sms, s);
-    return a.D <= 128 ? launch<128>(p, tq, tk, tv, to, sms, s) : launch<256>(p, tq, tk, tv, to, sms, s);
+    p.items = d.items;
+    p.whole = d.whole;
+    p.splits = d.splits;
+    const uint32_t heads = d.grid / (uint32_t)p.q_items;
+    p.dq = (int)(d.grid % (uint32_t)p.q_items);
+    p.dh = (int)(heads % (uint32_t)p.Hkv);
+    p.db = (int)(heads / (uint32_t)p.Hkv);
+    if (a.D <= 64) return launch<64>(d, p, tq, tk, tv, to, s);
+    return a.D <= 128 ? launch<128>(d, p, tq, tk, tv, to, s) : launch<256>(d, p, tq, tk, tv, to, s);
 }
 
 }  // namespace vd
