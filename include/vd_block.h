@@ -51,10 +51,16 @@ typedef struct {
 VD_API vd_status vd_op_cross_attention(const vd_xattn_desc* d, const void* q, const void* k, const void* v,
                                        const int32_t* kv_lens, void* o, void* cuda_stream);
 
-/* Test hook: how a bf16 call of the tensor-core kernel (aligned tensors) is shared out on the current device: of its `items` (up to 256
- * rows of a key head) the first `whole` are a thread block's each, the others a cluster's of `splits` blocks, which divide the keys.
- * VD_ERR_UNSUPPORTED where another kernel takes the call.  Launches nothing. */
-VD_API vd_status vd_debug_xattn_division(const vd_xattn_desc* d, int32_t* splits, int64_t* items, int64_t* whole);
+/* Test hooks.
+ *   vd_debug_xattn_division       how a bf16 call of the tensor-core kernel (aligned tensors) is shared out on the current device: of its
+ *                                 `items` (up to 256 rows of a key head) the first `whole` are a thread block's each, in turn over the `blocks` launched, the
+ *                                 others a cluster's of `splits` blocks, which divide the keys.  VD_ERR_UNSUPPORTED where
+ *                                 another kernel takes the call.  Launches nothing.
+ *   vd_debug_xattn_meeting_limit  SM clocks that blocks of a cluster wait for one another in the calls that follow, process-wide; 0: as many
+ *                                 as the call needs (the default); negative: they give up at once, as if the others did not come, and the
+ *                                 divided rows are NaN. */
+VD_API vd_status vd_debug_xattn_division(const vd_xattn_desc* d, int32_t* splits, int64_t* items, int64_t* whole, int64_t* blocks);
+VD_API vd_status vd_debug_xattn_meeting_limit(int64_t cycles);
 
 /* ------------------------------------------------------------------------------------------
  * Rotary positions.  The first rotary_dim channels of a head are rotary_dim / 2 pairs; pair i of a token turns by

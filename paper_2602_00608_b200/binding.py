@@ -35,7 +35,7 @@ EXPORTED = [
     "vd_last_error", "vd_destroy", "vd_num_steps", "vd_get_step", "vd_profile", "vd_debug_stop_after",
     "vd_conv_packed_weight_bytes", "vd_conv_pack_weight", "vd_op_conv2d", "vd_conv_route", "vd_op_conv2d_ex", "vd_conv_record_slots", "vd_op_merge_records", "vd_conv_stats_scratch_bytes", "vd_op_conv2d_stats", "vd_gn_scratch_bytes", "vd_op_gn_stats", "vd_op_gn_stats_single",
     "vd_op_attention", "vd_attention_scratch_bytes", "vd_op_gn_stats_static", "vd_clear_status", "vd_decode_host_stream", "vd_debug_check_canaries", "vd_debug_status_offset", "vd_debug_wait_probe",
-    "vd_op_cross_attention", "vd_op_rotary", "vd_rotary_frequencies", "vd_op_gate_norm", "vd_debug_xattn_division",
+    "vd_op_cross_attention", "vd_op_rotary", "vd_rotary_frequencies", "vd_op_gate_norm", "vd_debug_xattn_division", "vd_debug_xattn_meeting_limit",
 ]
 
 
@@ -158,7 +158,8 @@ def lib():
         l.vd_attention_scratch_bytes.argtypes = [c_int32, c_int32, c_int32]
         l.vd_attention_scratch_bytes.restype = c_size_t
         l.vd_op_cross_attention.argtypes = [POINTER(VdXattnDesc), vp, vp, vp, vp, vp, vp]
-        l.vd_debug_xattn_division.argtypes = [POINTER(VdXattnDesc), POINTER(c_int32), POINTER(c_int64), POINTER(c_int64)]
+        l.vd_debug_xattn_division.argtypes = [POINTER(VdXattnDesc), POINTER(c_int32), POINTER(c_int64), POINTER(c_int64), POINTER(c_int64)]
+        l.vd_debug_xattn_meeting_limit.argtypes = [c_int64]
         l.vd_op_rotary.argtypes = [POINTER(VdRotaryDesc), vp, vp, vp, vp, vp]
         l.vd_rotary_frequencies.argtypes = [POINTER(VdRotaryFreqDesc), POINTER(c_double)]
         l.vd_op_gate_norm.argtypes = [POINTER(VdGateNormDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
@@ -632,16 +633,16 @@ def op_cross_attention(q, k, v, kv_lens=None, scale=None, out=None, impl=VD_XATT
 
 
 def xattn_division(q, k, v):
-    """(splits, items, whole) of op_cross_attention(q, k, v) (see vd_debug_xattn_division), or None where another kernel takes it."""
+    """(splits, items, whole, blocks) of op_cross_attention(q, k, v) (see vd_debug_xattn_division), or None where another kernel takes it."""
     import torch
     desc = _describe_cross_attention(q, k, v, None, None, torch.empty_like(q, memory_format=torch.contiguous_format), VD_XATTN_AUTO)
-    splits, items, whole = c_int32(), c_int64(), c_int64()
+    splits, items, whole, blocks = c_int32(), c_int64(), c_int64(), c_int64()
     with torch.cuda.device(q.device):
-        status = lib().vd_debug_xattn_division(byref(desc), byref(splits), byref(items), byref(whole))
+        status = lib().vd_debug_xattn_division(byref(desc), byref(splits), byref(items), byref(whole), byref(blocks))
     if status == VD_ERR_UNSUPPORTED:
         return None
     _check(status)
-    return splits.value, items.value, whole.value
+    return splits.value, items.value, whole.value, blocks.value
 
 
 def rotary_frequencies(rotary_dim: int, base: float = 10000.0, *, axis_pairs=None, scaling=VD_ROTARY_SCALE_NONE, factor: float = 1.0,

@@ -94,9 +94,9 @@ vd_status vd_op_cross_attention(const vd_xattn_desc* d, const void* q, const voi
     return done(launch(a, (cudaStream_t)cuda_stream), "vd_op_cross_attention");
 }
 
-vd_status vd_debug_xattn_division(const vd_xattn_desc* d, int32_t* splits, int64_t* items, int64_t* whole) {
+vd_status vd_debug_xattn_division(const vd_xattn_desc* d, int32_t* splits, int64_t* items, int64_t* whole, int64_t* blocks) {
     if (const char* e = xattn_error(d)) return refuse(VD_ERR_INVALID_ARG, e);
-    if (!splits || !items || !whole) return refuse(VD_ERR_INVALID_ARG, "NULL pointer");
+    if (!splits || !items || !whole || !blocks) return refuse(VD_ERR_INVALID_ARG, "NULL pointer");
     const uintptr_t at = 4096;
     const XAttnArgs a = xattn_args(d, (void*)at, (void*)at, (void*)at, nullptr, (void*)at);
     if (d->batch == 0 || d->q_len == 0 || d->impl != VD_XATTN_AUTO || kernel_of(a) != launch_xattn_tc)
@@ -107,6 +107,12 @@ vd_status vd_debug_xattn_division(const vd_xattn_desc* d, int32_t* splits, int64
     *splits = div.splits;
     *items = div.items;
     *whole = div.whole;
+    *blocks = div.grid;
+    return VD_OK;
+}
+
+vd_status vd_debug_xattn_meeting_limit(int64_t cycles) {
+    xattn_tc_meeting_limit(cycles);
     return VD_OK;
 }
 

@@ -26,6 +26,7 @@ bool xattn_tc_supported(const XAttnArgs& a);
 cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s);
 struct XAttnDivision { int splits; uint32_t items, whole, grid; };       // the first `whole` items are a CTA's each, the others a cluster's of `splits` CTAs
 cudaError_t xattn_tc_division(const XAttnArgs& a, XAttnDivision* d);
+void xattn_tc_meeting_limit(long long cycles);
 
 struct RotaryArgs {
     const void* x; void* y;

@@ -132,6 +132,13 @@ template <int N> __device__ __forceinline__ void bulk_wait_group() {
 __device__ __forceinline__ void named_barrier_sync(int id, int count) {
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(count) : "memory");
 }
+// the same, and whether `ok` holds for all of them
+__device__ __forceinline__ bool named_barrier_all(int id, int count, bool ok) {
+    uint32_t all;
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 q, %3, 0;\nbarrier.cta.red.and.pred p, %1, %2, q;\nselp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(all) : "r"(id), "r"(count), "r"((uint32_t)ok) : "memory");
+    return all != 0u;
+}
 __device__ __forceinline__ void named_barrier_arrive(int id, int count) {
     asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(count) : "memory");
 }

@@ -19,10 +19,12 @@
 // chain of scores, maximum, exponentials and product, which two tiles overlap and tensor memory has no room for a third.
 // Keys behind a row's length: scores are replaced before the maximum, P is zero there, and the up to 15 rows of V that the last
 // product still reads are zeroed in shared memory, since 0 * NaN is NaN.
-// Every wait is bounded (see tc_common.cuh); rows of an item whose wait gave up are NaN.
+// Every wait is bounded (see tc_common.cuh; where CTAs wait for one another the bound grows with the keys); rows of an item whose wait gave
+// up are NaN.
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "block_ops.h"
 #include "conv_cluster.cuh"
@@ -61,7 +63,7 @@ template <int DP, bool SHORT = false> struct Cfg {
 };
 struct Bars {
     uint64_t q_full[2], q_empty[2], full[6], empty[6], s_full[2], s_free[2], p_part[2][2], pv_done[2], o_full[2], drained[2], shown[2], seen[2], o_left;
-    uint32_t tmem_base, abort_flag;
+    uint32_t tmem_base, abort_flag, lost[2];                 // lost: a wait at a meeting of tile s gave up
 };
 static_assert(sizeof(Bars) <= 320 && Cfg<256>::SMEM <= 232448 && Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448 && 2 * (Cfg<64, true>::SMEM + 1024) <= 233472, "shared memory of one CTA");
 
@@ -76,6 +78,8 @@ struct Params {
     __nv_bfloat16* o;
     int64_t o_batch, o_token, o_head;
     float scale_log2, scale_far;     // scale_far: the power of two at or above it (Scaled)
+    long long wait_limit;            // cycles, where CTAs wait for one another (launch_xattn_tc)
+    long long meeting_limit;         // the same at meetings; negative: they give up at once (a test's)
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -170,17 +174,14 @@ template <int DP> struct Tile {
     float m_ref;
     unsigned long long sum, sum_b;       // of even and odd pairs of keys
     bool ok = true;
-    float limit;                         // what a score is looked at beyond (refer)
 
+    __device__ __forceinline__ float scale() const { return fabsf(m_ref) > FAR ? to_log2.far : to_log2.near; }
     // What the exponentials are relative to: at first the maximum itself, whose P is then 1 and is not rounded (a row that one key has, or all
     // but has, is that key's value).  It stays unless a score exceeds it by more than the threshold, and moves by a whole number, so
     // that what has been summed (O, the sums, P as far as it is written) is rescaled by a power of two, without rounding.
-    __device__ __forceinline__ float scale() const { return fabsf(m_ref) > FAR ? to_log2.far : to_log2.near; }
-    // A far reference, or none yet: every score is looked at.  (The scale in a register of its own beside the limit: 8 x 1350 x 1350, 30 heads of
-    // 64 192.8 us instead of 184.8.)
-    __device__ __forceinline__ void refer() { limit = fabsf(m_ref) > FAR ? -INFINITY : m_ref + RESCALE_THRESHOLD; }
     __device__ __forceinline__ void move_reference(float score, uint32_t p_cols) {
-        if (!__any_sync(0xffffffffu, score * to_log2.near > limit)) return;
+        // (a far reference, or none yet: every score is looked at closely; score() for every tile: 5400 x 14400, 16 heads of 128 540 us instead of 522)
+        if (!__any_sync(0xffffffffu, score * to_log2.near > (fabsf(m_ref) > FAR ? -INFINITY : m_ref + RESCALE_THRESHOLD))) return;
         const float top = to_log2.score(score);
         const bool grow = top > m_ref + RESCALE_THRESHOLD;
         float factor = 1.f;
@@ -189,7 +190,6 @@ template <int DP> struct Tile {
             factor = by < 127.f ? __int_as_float((127 - (int)by) << 23) : 0.f;
             m_ref = by < 127.f ? m_ref + by : top;
         }
-        refer();
         if (!__any_sync(0xffffffffu, grow)) return;
         sum = fmaf2(sum, pack2(factor, factor), 0ull);
         sum_b = fmaf2(sum_b, pack2(factor, factor), 0ull);
@@ -234,7 +234,6 @@ template <int DP> struct Tile {
     // a score is.
     __device__ __forceinline__ float full(uint64_t* first_half) {
         uint32_t a[32], b[32], c[32];
-        refer();
         tmem_ld32(t_s, a);
         tmem_ld32(t_s + 32u, b);
         tmem_ld32(t_s + 64u, c);
@@ -261,7 +260,6 @@ template <int DP> struct Tile {
     // The same where only the first `valid` <= 96 keys count: the others leave before the maximum, 16 keys are the least that is worked on.
     __device__ __forceinline__ float most(int valid, uint64_t* first_half) {
         uint32_t a[32], b[32], c[32];
-        refer();
         tmem_ld32(t_s, a);
         tmem_ld32(t_s + 32u, b);
         tmem_ld32(t_s + 64u, c);
@@ -292,7 +290,6 @@ template <int DP> struct Tile {
     // The same for any number of them, 32 at a time.  (The code of full() with masks spills.)
     __device__ __forceinline__ float part(int valid, uint64_t* first_half) {
         uint32_t r[32];
-        refer();
         float top = -INFINITY;
 #pragma unroll 1
         for (int c = 0; c < valid; c += 32) {
@@ -410,24 +407,32 @@ __device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
     asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
     return v;
 }
+__device__ __forceinline__ bool heard(const Params& a, uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
+    if (a.meeting_limit < 0) {
+        *abort_flag = 1;
+        return false;
+    }
+    return cc::wait_cluster(smem_u32(bar), parity, abort_flag, a.meeting_limit);
+}
 // The CTAs of a cluster have each taken a share of an item's keys: they show one another half of the channels at a time, in fp32, and each
 // adds up (in the order of the shares) and writes its part of the tile's rows.  By the 128 threads of tile s; `rounds` counts what these
-// have shown so far.  A load of another CTA's memory takes 900 cycles.  FAST: a thread has a row, its weights in registers and all shares'
-// loads under way at once (18000 instead of 29000 cycles a meeting), which crowds the softmax's
-// registers: calls with whole items besides take the loops, out of line (5400 x 14400, 16 heads of 128 519 us, FAST 546).
+// have shown so far.  Once a wait gave up the others are told nothing more, so that they give up too and nobody takes old or half-written shares
+// for an item's: what a CTA still writes is NaN.  A load of another CTA's memory takes 900 cycles.  FAST: a thread has a row, its weights in
+// registers and all shares' loads under way at once (18000 instead of 29000 cycles a meeting), which crowds the softmax's registers: calls with
+// whole items besides take the loops, out of line (5400 x 14400, 16 heads of 128 519 us, FAST 546).
 template <int DP, bool FAST>
 __device__ __forceinline__ void meet_inline(const Params& a, const Items<true>& it, Bars* bars, uint8_t* show, float2* ml, float2 mine, uint32_t t_o, int s, int row, uint32_t rounds) {
     constexpr int COLS = DP / 2, PIECES = COLS / 4;          // of a round; 16-byte pieces of them
     volatile uint32_t* abort_flag = &bars->abort_flag;
     const int rank = (int)cluster_ctarank();
+    volatile uint32_t* lost = &bars->lost[s];
+    bool ok = true;
     auto tell = [&](uint64_t* bar) {
+        if (!ok) *lost = 1;                                  // (read behind the barrier; as barrier.red of `ok` the meetings took 2 us more)
         named_barrier_sync(1 + s, ROWS);
-        if (row < a.splits) arrive_release_cluster(map_to_cta(smem_u32(bar), (uint32_t)row));
+        if (row < a.splits && !*lost) arrive_release_cluster(map_to_cta(smem_u32(bar), (uint32_t)row));
     };
-    auto hear = [&](uint64_t* bar, uint32_t parity) {
-        (void)cc::wait_cluster(smem_u32(bar), parity, abort_flag);
-        __syncwarp();
-    };
+    auto hear = [&](uint64_t* bar, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && !*lost && heard(a, bar, parity, abort_flag)); };
     const int r0 = ROWS * rank / a.splits, r1 = ROWS * (rank + 1) / a.splits;
     // FAST: this thread's row of the CTA's part, and how many threads it has
     const int per_row = ROWS / ((ROWS + a.splits - 1) / a.splits), r = r0 + row / per_row, tt = r / a.g, t = it.t0 + s * a.nt + tt;
@@ -436,20 +441,22 @@ __device__ __forceinline__ void meet_inline(const Params& a, const Items<true>& 
     float f[MAX_SPLITS];                                     // the shares' weights
     for (int round = 0; round < 2; ++round, ++rounds) {
         if (rounds > 0) hear(&bars->seen[s], (rounds - 1) & 1);      // everybody has read what was shown last
-        if (round == 0) ml[row] = mine;
+        if (ok) {                                           // (the same for a warp)
+            if (round == 0) ml[row] = mine;
 #pragma unroll
-        for (int c = 0; c < COLS; c += 32) {
-            uint32_t v[32];
-            if (it.n) {
-                tmem_ld32(t_o + (uint32_t)(round * COLS + c), v);
-                tmem_ld_wait();
-            } else {
+            for (int c = 0; c < COLS; c += 32) {
+                uint32_t v[32];
+                if (it.n) {
+                    tmem_ld32(t_o + (uint32_t)(round * COLS + c), v);
+                    tmem_ld_wait();
+                } else {
 #pragma unroll
-                for (int q = 0; q < 32; ++q) v[q] = 0u;
+                    for (int q = 0; q < 32; ++q) v[q] = 0u;
+                }
+#pragma unroll
+                for (int q = 0; q < 32; q += 4)
+                    *(uint4*)(show + row * (COLS * 4) + ((((c + q) >> 2) ^ (row & (PIECES - 1))) << 4)) = make_uint4(v[q], v[q + 1], v[q + 2], v[q + 3]);
             }
-#pragma unroll
-            for (int q = 0; q < 32; q += 4)
-                *(uint4*)(show + row * (COLS * 4) + ((((c + q) >> 2) ^ (row & (PIECES - 1))) << 4)) = make_uint4(v[q], v[q + 1], v[q + 2], v[q + 3]);
         }
         tell(&bars->shown[s]);
         hear(&bars->shown[s], rounds & 1);
@@ -472,6 +479,9 @@ __device__ __forceinline__ void meet_inline(const Params& a, const Items<true>& 
                 for (int k = 0; k < MAX_SPLITS; ++k)
                     if (k < a.splits) f[k] /= l;
             }
+            if (!ok)
+#pragma unroll
+                for (int k = 0; k < MAX_SPLITS; ++k) f[k] = __int_as_float(0x7fffffff);
             for (int piece = row % per_row; piece < PIECES; piece += per_row) {
                 const int d = round * COLS + piece * 4;
                 if (d >= a.D) break;
@@ -508,7 +518,7 @@ __device__ __forceinline__ void meet_inline(const Params& a, const Items<true>& 
                 l = fmaf(f, w.y, l);
                 o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
             }
-            const float inv = 1.f / l;
+            const float inv = ok ? 1.f / l : __int_as_float(0x7fffffff);
             *(uint2*)(a.o + it.b * a.o_batch + t * a.o_token + (it.kvh * a.g + r - tt * a.g) * a.o_head + d) =
                 make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
         }
@@ -519,6 +529,19 @@ __device__ __forceinline__ void meet_inline(const Params& a, const Items<true>& 
 template <int DP>
 __device__ __noinline__ void meet_out_of_line(const Params& a, const Items<true>& it, Bars* bars, uint8_t* show, float2* ml, float2 mine, uint32_t t_o, int s, int row, uint32_t rounds) {
     meet_inline<DP, false>(a, it, bars, show, ml, mine, t_o, s, row, rounds);
+}
+// Before the rows of a divided item without keys: what was shown at the last meeting has been read.  If it may not have been, they leave straight
+// from the threads: false.
+__device__ __noinline__ bool seen_or_zeros(const Params& a, const Items<true>& it, Bars* bars, int s, int row, uint32_t rounds) {
+    bool ok = !*(volatile uint32_t*)&bars->lost[s];
+    ok = __all_sync(0xffffffffu, ok && heard(a, &bars->seen[s], (rounds - 1) & 1, &bars->abort_flag));
+    if (named_barrier_all(1 + s, ROWS, ok)) return true;
+    bars->lost[s] = 1;
+    const int tt = row / a.g, t = it.t0 + s * a.nt + tt;
+    if (tt < a.nt && t < a.Tq)
+        for (int d = 0; d < a.D; d += 8)
+            *(uint4*)(a.o + it.b * a.o_batch + t * a.o_token + (it.kvh * a.g + row - tt * a.g) * a.o_head + d) = make_uint4(0, 0, 0, 0);
+    return false;
 }
 
 // DIVIDED: by keys among the CTAs of a cluster are no items, those that whole rounds leave over, or all (builds of their own: the code costs
@@ -552,7 +575,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
         }
         for (int i = 0; i < C::STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), C::MMA_WARPS); }
         mbar_init(smem_u32(&bars->o_left), 1);
-        bars->abort_flag = 0;
+        bars->abort_flag = bars->lost[0] = bars->lost[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async_smem();
     }
@@ -616,9 +639,8 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
             // the rows through shared memory (swizzled like the operands), out by a bulk tensor store that the next item's softmax does not wait
             // for: rows written straight from the threads, a line each, held the load/store unit for 2000 cycles an item
             if (out_thread) bulk_wait_group_read<0>();       // the last item's rows have left
-            if (SPLIT && n_meet) {                           // and what was shown at the last meeting has been read
-                (void)cc::wait_cluster(smem_u32(&bars->seen[s]), (n_meet - 1) & 1, abort_flag);
-                __syncwarp();
+            if constexpr (SPLIT) {
+                if (n_meet && !seen_or_zeros(a, it, bars, s, row, n_meet)) continue;
             }
             named_barrier_sync(1 + s, ROWS);
 #pragma unroll
@@ -667,7 +689,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
                 if (!ok) break;
                 if (!it.n) continue;
                 const int buf = q_issued % C::Q_BUFS;
-                ok = mbar_wait(smem_u32(&bars->q_empty[buf]), ((q_issued / C::Q_BUFS) & 1) ^ 1, abort_flag);
+                ok = mbar_wait(smem_u32(&bars->q_empty[buf]), ((q_issued / C::Q_BUFS) & 1) ^ 1, abort_flag, SPLIT ? a.wait_limit : WAIT_LIMIT_CYCLES);
                 if (!ok) break;
                 const uint32_t qf = smem_u32(&bars->q_full[buf]);
                 mbar_arrive_expect_tx(qf, (uint32_t)(it.streams * C::CHUNKS * a.g * a.nt * 128));
@@ -676,7 +698,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
                         tma_load_5d(smem_u32(smem_q + (buf * 2 + s) * C::TILE_BYTES + c * (ROWS * 128)), &tm_q, c * CHUNK, 0, it.t0 + s * a.nt, it.kvh, it.b, qf);
                 ++q_issued;
                 for (int j = 0; j < 2 * it.n && ok; ++j) {
-                    ok = mbar_wait(smem_u32(&bars->empty[st]), ph ^ 1, abort_flag);
+                    ok = mbar_wait(smem_u32(&bars->empty[st]), ph ^ 1, abort_flag, SPLIT ? a.wait_limit : WAIT_LIMIT_CYCLES);
                     if (!ok) break;
                     const uint32_t full = smem_u32(&bars->full[st]);
                     mbar_arrive_expect_tx(full, C::TILE_BYTES);
@@ -694,7 +716,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
             }
             // Everything has landed once it has been multiplied; if a wait gave up anywhere, before the CTA's memory goes.
             for (int k = 0; k < C::STAGES && ok; ++k) {
-                ok = mbar_wait(smem_u32(&bars->empty[st]), ph ^ 1, abort_flag);
+                ok = mbar_wait(smem_u32(&bars->empty[st]), ph ^ 1, abort_flag, SPLIT ? a.wait_limit : WAIT_LIMIT_CYCLES);
                 if (ok && ++st == C::STAGES) { st = 0; ph ^= 1; }
             }
             if (!ok) {
@@ -715,7 +737,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
         uint32_t st = 0, ph = 0, n_q = 0;
         auto wait_on = [&](uint64_t* bar, uint32_t parity) {
             const uint32_t p = smem_u32(bar);
-            if (!mbar_try_wait(p, parity)) (void)mbar_wait(p, parity, abort_flag);
+            if (!mbar_try_wait(p, parity)) (void)mbar_wait(p, parity, abort_flag, SPLIT ? a.wait_limit : WAIT_LIMIT_CYCLES);
             tc_fence_after();
         };
         auto commit = [&](uint64_t* bar) { umma_commit_on(smem_u32(bar), on); };
@@ -910,6 +932,8 @@ template <int DP> cudaError_t launch(const XAttnDivision& d, const Params& p, co
     return launch_as<DP, NONE>(d, p, tq, tk, tv, to, s);
 }
 
+std::atomic<long long> meeting_limit{0};                      // a test's; 0: by the call
+
 int items_of_head(const XAttnArgs& a) {                      // tiles of nt tokens, two to an item (one beyond 128 channels)
     const int tokens = (a.D > 128 ? 1 : 2) * (ROWS / (a.H / a.Hkv));
     return (a.Tq + tokens - 1) / tokens;
@@ -926,6 +950,8 @@ bool xattn_tc_supported(const XAttnArgs& a) {
     };
     return kv_maps_supported(a, 256) && g <= ROWS && rows_ok(a.q, a.sq) && rows_ok(a.o, a.so);
 }
+
+void xattn_tc_meeting_limit(long long cycles) { meeting_limit.store(cycles, std::memory_order_relaxed); }
 
 cudaError_t xattn_tc_division(const XAttnArgs& a, XAttnDivision* d) {
     int dev = 0, sms = 0;
@@ -956,6 +982,12 @@ cudaError_t launch_xattn_tc(const XAttnArgs& a, cudaStream_t s) {
     p.items = d.items;
     p.whole = d.whole;
     p.splits = d.splits;
+    // A CTA may come to its first meeting behind all its whole items while another of its cluster had none with keys, and its other roles wait meanwhile:
+    // the limit grows by what as many tiles may take, at 16384 cycles each (2000 to 3000 as measured).
+    const int64_t rounds = d.splits > 1 ? d.whole / d.grid + 1 : 0, tiles = (a.Tk + KEYS - 1) / KEYS;
+    p.wait_limit = tc::WAIT_LIMIT_CYCLES + rounds * tiles * 16384;
+    const long long asked = meeting_limit.load(std::memory_order_relaxed);
+    p.meeting_limit = asked ? asked : p.wait_limit;
     const uint32_t heads = d.grid / (uint32_t)p.q_items;
     p.dq = (int)(d.grid % (uint32_t)p.q_items);
     p.dh = (int)(heads % (uint32_t)p.Hkv);
