@@ -77,7 +77,7 @@ typedef enum {
 typedef struct {
     uint32_t struct_size;
     int32_t dtype;              /* vd_dtype of x and y */
-    int32_t batch, tokens, heads;       /* >= 0; batch * tokens < 2^31 */
+    int32_t batch, tokens, heads;       /* >= 0; batch * tokens < 2^31, heads at most 2^30 */
     int32_t head_dim;           /* 1..1024 */
     int32_t rotary_dim;         /* even, 0..head_dim */
     int32_t layout;             /* vd_rotary_layout */

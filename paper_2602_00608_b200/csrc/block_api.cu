@@ -158,7 +158,7 @@ vd_status vd_op_rotary(const vd_rotary_desc* d, const void* x, const int32_t* po
     if (!d) return refuse(VD_ERR_INVALID_ARG, "NULL descriptor");
     if (d->struct_size != sizeof(vd_rotary_desc)) return refuse(VD_ERR_INVALID_ARG, "vd_rotary_desc: struct_size mismatch");
     if (!is_dtype(d->dtype)) return refuse(VD_ERR_INVALID_ARG, "bad dtype");
-    if (d->batch < 0 || d->tokens < 0 || d->heads < 0 || d->head_dim < 1 || d->head_dim > 1024 || d->rotary_dim > d->head_dim || !fits(d->batch, d->tokens, 1))
+    if (d->batch < 0 || d->tokens < 0 || d->heads < 0 || d->heads > 1 << 30 || d->head_dim < 1 || d->head_dim > 1024 || d->rotary_dim > d->head_dim || !fits(d->batch, d->tokens, 1))
         return refuse(VD_ERR_INVALID_ARG, "bad rotary sizes");
     if (const char* e = rotary_axes_error(d->rotary_dim, d->axes, d->axis_pairs)) return refuse(VD_ERR_INVALID_ARG, e);
     if (d->layout != VD_ROTARY_HALF && d->layout != VD_ROTARY_INTERLEAVED) return refuse(VD_ERR_INVALID_ARG, "bad layout");

@@ -195,3 +195,11 @@ def test_cross_attention_refuses_an_output_that_is_an_input(which):
     at = [ctypes.c_void_p(4096 * (i + 1)) for i in range(3)]
     assert vd.lib().vd_op_cross_attention(ctypes.byref(xattn()), *at, None, at[which], None) == vd.VD_ERR_INVALID_ARG
     assert b"o is an input" in vd.lib().vd_last_error(None)
+
+
+@pytest.mark.parametrize("heads", [(1 << 30) + 1, (1 << 31) - 1])
+def test_rotary_refuses_heads_that_would_wrap(heads):
+    """A thread steps over the heads by up to 1024: an int32 would turn negative behind the last of 2^31 - 1, and the thread go on there."""
+    far = dict(batch=1, tokens=1, heads=heads, head_dim=8, rotary_dim=8, axis_pairs=(4, 0, 0, 0), x_head=0, y_head=8, y_token=8 * heads, y_batch=8 * heads)
+    assert vd.lib().vd_op_rotary(ctypes.byref(rotary(**far)), P, P, P, ctypes.c_void_p(1 << 20), None) == vd.VD_ERR_INVALID_ARG
+    assert b"rotary sizes" in vd.lib().vd_last_error(None)
