@@ -40,7 +40,7 @@ typedef struct {
     int32_t heads, kv_heads;    /* heads a multiple of kv_heads */
     int32_t head_dim;           /* 1..256 */
     int32_t impl;               /* vd_xattn_impl */
-    float scale;                /* > 0, finite */
+    float scale;                /* > 0, at most 2^126 */
     int64_t q_batch, q_token, q_head;
     int64_t k_batch, k_token, k_head;
     int64_t v_batch, v_token, v_head;

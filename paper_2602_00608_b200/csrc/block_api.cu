@@ -51,7 +51,7 @@ const char* xattn_error(const vd_xattn_desc* d) {
         (int64_t)d->batch * d->heads * d->q_len > 1 << 30)
         return "bad attention sizes";
     if (d->impl < VD_XATTN_AUTO || d->impl > VD_XATTN_PLAIN) return "bad impl";
-    if (!(d->scale > 0.f) || isinf(d->scale)) return "scale must be positive and finite";
+    if (!(d->scale > 0.f && d->scale <= 8.5070592e37f)) return "scale must be positive, at most 2^126";     // (times log2 e it is still finite)
     if (!not_negative(&d->q_batch, 12)) return "negative stride";
     return nullptr;
 }

@@ -203,3 +203,12 @@ def test_rotary_refuses_heads_that_would_wrap(heads):
     far = dict(batch=1, tokens=1, heads=heads, head_dim=8, rotary_dim=8, axis_pairs=(4, 0, 0, 0), x_head=0, y_head=8, y_token=8 * heads, y_batch=8 * heads)
     assert vd.lib().vd_op_rotary(ctypes.byref(rotary(**far)), P, P, P, ctypes.c_void_p(1 << 20), None) == vd.VD_ERR_INVALID_ARG
     assert b"rotary sizes" in vd.lib().vd_last_error(None)
+
+
+def test_cross_attention_refuses_scales_that_overflow_in_units_of_log_2():
+    l = vd.lib()
+    for scale in (8.6e37, 3e38):
+        assert l.vd_op_cross_attention(ctypes.byref(xattn(scale=scale)), P, P, P, None, ctypes.c_void_p(1 << 20), None) == vd.VD_ERR_INVALID_ARG
+        assert b"scale" in l.vd_last_error(None)
+    for scale in (2.0 ** 126, 1e-45):
+        assert l.vd_op_cross_attention(ctypes.byref(xattn(scale=scale, batch=0)), None, None, None, None, None, None) == vd.VD_OK
