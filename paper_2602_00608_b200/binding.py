@@ -608,7 +608,7 @@ def _describe_cross_attention(q, k, v, kv_lens, scale, out, impl):
     sq, sk, sv, so = q.stride(), k.stride(), v.stride(), out.stride()
     if d > 1 and not sq[3] == sk[3] == sv[3] == so[3] == 1:
         _refuse("the channels of a head must lie side by side")
-    return VdXattnDesc(ctypes.sizeof(VdXattnDesc), _block_dtype(q, "q"), b, tq, tk, h, hkv, d, impl, d ** -0.5 if scale is None else scale,
+    return VdXattnDesc(ctypes.sizeof(VdXattnDesc), _block_dtype(q, "q"), b, tq, tk, h, hkv, d, impl, (d or 1) ** -0.5 if scale is None else scale,
                        sq[0], sq[1], sq[2], sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], so[0], so[1], so[2])
 
 

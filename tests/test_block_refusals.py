@@ -212,3 +212,13 @@ def test_cross_attention_refuses_scales_that_overflow_in_units_of_log_2():
         assert b"scale" in l.vd_last_error(None)
     for scale in (2.0 ** 126, 1e-45):
         assert l.vd_op_cross_attention(ctypes.byref(xattn(scale=scale, batch=0)), None, None, None, None, None, None) == vd.VD_OK
+
+
+def test_heads_without_channels_are_refused_by_the_library(monkeypatch):
+    """Where no scale is given one follows from the number of channels, which may be none."""
+    import torch
+    monkeypatch.setattr(vd, "_on_device", lambda *a, **kw: None)
+    x = torch.zeros(1, 2, 2, 0)
+    desc = vd._describe_cross_attention(x, x, x, None, None, x, vd.VD_XATTN_AUTO)
+    assert vd.lib().vd_op_cross_attention(ctypes.byref(desc), P, P, P, None, ctypes.c_void_p(1 << 20), None) == vd.VD_ERR_INVALID_ARG
+    assert b"sizes" in vd.lib().vd_last_error(None)
