@@ -302,19 +302,19 @@ template <typename XT, typename HT> cudaError_t launch_typed(const GateNormArgs&
         if (vecs <= 1024) return launch<XT, HT, 8, 512, 2>(a, s);
         return launch<XT, HT, 8, 512, 4>(a, s);
     }
-    // (920 tokens of 4436, bf16, norms on both sides: one channel at a time 49 us, two 21)
     const uint64_t even = d.x_batch | d.x_token | (a.x_out ? d.xo_batch | d.xo_token : 0) | (a.h ? d.h_batch | d.h_token : 0) |
                           (a.y ? d.y_batch | d.y_token : 0) | (a.gate ? d.gate_batch | d.gate_group : 0) |
                           (a.scale ? d.scale_batch | d.scale_group : 0) | (a.shift ? d.shift_batch | d.shift_group : 0);
     const uint64_t x_at = (uintptr_t)a.x | (uintptr_t)a.x_out, f_at = (uintptr_t)a.weight | (uintptr_t)a.bias | (uintptr_t)a.post_weight,
                    h_at = (uintptr_t)a.h | (uintptr_t)a.y | (uintptr_t)a.gate | (uintptr_t)a.scale | (uintptr_t)a.shift;
     if (C % 2 == 0 && even % 2 == 0 && x_at % (2 * xs) == 0 && h_at % (2 * hs) == 0 && f_at % 8 == 0) {
+        // (920 tokens of 4436, bf16, norms on both sides: one channel at a time 49 us, two 21.)  The fewest threads and then the fewest slots that hold a
+        // token, against the next step, us, 6.4 million values, norms on both sides, fp32 (bf16): 254 channels 24.8 / 49.6 (24.0 / 52.2), 1022 26.5 / 32.9
+        // (24.7 / 32.4), 2046 26.8 / 41.2 (25.6 / 41.2), 4098 30.2 / 44.6 (28.0 / 44.6), 5118 30.5 / 39.9 (28.3 / 39.2), 8190 37.1 / 42.3 (35.2 / 42.4)
         const int n = C / 2;
         if (n <= 128) return launch<XT, HT, 2, 32, 4>(a, s);
         if (n <= 512) return launch<XT, HT, 2, 128, 4>(a, s);
-        if (n <= 768) return launch<XT, HT, 2, 256, 3>(a, s);
         if (n <= 1024) return launch<XT, HT, 2, 256, 4>(a, s);
-        if (n <= 1536) return launch<XT, HT, 2, 512, 3>(a, s);
         if (n <= 2560) return launch<XT, HT, 2, 512, 5>(a, s);
         if (n <= 4096) return launch<XT, HT, 2, 512, 8>(a, s);
         return launch<XT, HT, 2, 512, MAX_CHANNELS / 1024>(a, s);
@@ -322,6 +322,10 @@ template <typename XT, typename HT> cudaError_t launch_typed(const GateNormArgs&
     // One channel at a time: the issue slots bound it (600 instructions for a warp's five channels), so few threads with many channels each, the
     // barriers, divisions and addresses being each warp's; but slots that find no channel cost too.  3039 tokens of 1111, fp32, norms on both
     // sides: 256 threads of eight 23.3 us, of five 18.6, 128 of nine 16.9; of 2401: 512 of five 51, 256 of ten 39; of 3501: 512 of seven 60, 256 of 14 62.
+    // Each step against the next at the widest token that it takes, us, 6.4 million values, norms on both sides, fp32 (bf16): 127 channels 30.5 / 82.2
+    // (29.9 / 86.3), 511 29.4 / 33.0 (29.8 / 33.0), 767 26.9 / 28.9 (27.5 / 30.8), 897 28.0 / 28.9 (29.4 / 30.2), 1151 26.4 / 27.1 (28.6 / 29.0), 1279
+    // 26.8 / 28.6 (28.7 / 31.4), 1535 26.8 / 32.9 (31.3 / 32.9), 2047 28.9 / 29.8 (30.3 / 33.1), 2559 28.8 / 39.2 (32.3 / 40.5), 3583 33.1 / 36.8
+    // (35.9 / 40.0), 5119 32.1 / 49.3 (36.1 / 54.0), 8191 43.2 / 53.4 (49.4 / 61.7).
     if (C <= 128) return launch<XT, HT, 1, 32, 4>(a, s);
     if (C <= 512) return launch<XT, HT, 1, 128, 4>(a, s);
     if (C <= 768) return launch<XT, HT, 1, 128, 6>(a, s);
