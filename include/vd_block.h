@@ -25,8 +25,14 @@ extern "C" {
  * Attention of many heads to states of another length:
  *   o[b,t,h,:] = sum_{u < len[b]} softmax_u(scale * q[b,t,h,:].k[b,u,h/g,:]) v[b,u,h/g,:],   g = heads / kv_heads
  * len = kv_lens clamped to 0..kv_len, or kv_len where kv_lens is NULL.  Keys and values at or behind len are never used,
- * whatever they hold; a row without keys is zeros.  Sums and the softmax are fp32; VD_BF16 rounds the result
- * to bf16 and may round the probabilities (relative to the row's largest).  Bitwise reproducible.
+ * whatever they hold; a row without keys is zeros; one whose scores are all minus infinity, or one of them NaN or plus infinity, is NaN.
+ * Sums and the softmax are fp32; VD_BF16 rounds the result to bf16 and may round the probabilities (relative to the row's
+ * largest).  Bitwise reproducible.
+ * Sums run over the keys in a row, relative to the largest score so far: |v| times the number of keys has to stay within fp32, and
+ * what falls off a running sum grows with the keys.  With equal scores, values of 1.3125 throughout and keys that are not divided
+ * among blocks (many rows or heads): bf16 exact at 2^20 keys, off by 1 % at 2^22 and 8 % at 2^24; fp32 by 3 % at 2^22.
+ * Waits inside the kernels are bounded (a second; where blocks wait for one another longer, by the keys).  None of them ends so unless
+ * the device or this library is at fault; the rows of the call that it concerns are then NaN, and there is no status to ask for.
  * ---------------------------------------------------------------------------------------- */
 typedef enum {
     VD_XATTN_AUTO = 0,

@@ -234,7 +234,8 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, V == 8 && TPR == 128 ? 
         }
 }
 
-// h, y and the modulation in types of their own: one channel at a time, types looked at per access
+// h, y and the modulation in types of their own: one channel at a time, types looked at per access, 32 slots of 512 threads whatever the width
+// (fp32 modulation of bf16 blocks, fp32 stream: 21600 x 1920 1410 us, with a bf16 modulation 87; 2700 x 16384 1082 and 140)
 constexpr int MIXED_THREADS = 512, MIXED_PER = MAX_CHANNELS / MIXED_THREADS;
 __global__ void __launch_bounds__(MIXED_THREADS) gate_norm_mixed_kernel(const GateNormArgs a) {
     __shared__ float red[2][MIXED_THREADS / 32];

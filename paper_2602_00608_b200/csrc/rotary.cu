@@ -102,7 +102,8 @@ __global__ void __launch_bounds__(MAX_THREADS) rotary_vec_kernel(const RotaryArg
     }
 }
 
-// any size and alignment: a block per token; thread-strided over (head, pair or copied channel)
+// any size and alignment: a block per token; thread-strided over (head, pair or copied channel).  (21600 tokens x 60 heads, bf16: of 40 in halves
+// 142 us, of 64 with 20 channels turned 304, of 64 at odd elements 211; in 16-byte pieces 64 takes 52.)
 __global__ void __launch_bounds__(MAX_THREADS) rotary_kernel(const RotaryArgs a) {
     extern __shared__ float2 table[];                        // of the token's pairs
     const int b = (int)(blockIdx.x / (uint32_t)a.T), t = (int)(blockIdx.x % (uint32_t)a.T), pairs = a.R / 2, work = pairs + a.D - a.R;

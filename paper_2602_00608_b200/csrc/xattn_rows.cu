@@ -6,9 +6,9 @@
 // The running maximum is a warp's, moved only when a score exceeds it by 2^8 (every lane's sums share it, so they add without
 // weights).  With more rows the arithmetic is what bounds this, and bf16 takes matrix instructions instead (below).  Warps meet in shared memory;
 // where there are few heads, a cluster of up to eight CTAs divides the keys and meets in distributed shared memory.  Fixed orders throughout:
-// the same bits each time.  4 sequences of up to 16384 keys, 8 key heads of 128 with 4 rows each: 218 MB in 40 us, 5.5 TB/s with the launch and
-// the meeting, DRAM 70 % busy.  Eight warps a CTA (16 warps: 8 x 16 heads, 512 keys of 64 6.9 -> 6.5 us, but 256 x 2000 of 128 43.5 -> 46.4 and
-// fp32, 512 x 1000 of 64 30.0 -> 35.2; 4 warps: 8.5, 44.6, 25.0, but fp32, 32 x 4096 of 80 20.7 -> 26.4).
+// the same bits each time.  4 sequences of up to 16384 keys, 8 key heads of 128 with 4 rows each: 218 MB in 41 us, 5.3 TB/s with the launch and
+// the meeting, DRAM 70 % busy.  Eight warps a CTA (us, 4 / 8 / 16 warps: 8 x 16 heads, 512 keys of 64 8.5 / 6.5 / 8.5; 256 x 2000 of 128
+// 45.0 / 43.3 / 58.3; fp32, 512 x 1000 of 64 42.9 / 43.4 / 47.5, 32 x 4096 of 80 26.5 / 20.1 / 24.9).
 #include "block_ops.h"
 #include "xattn_maps.h"
 #include "xattn_meet.cuh"

@@ -11,11 +11,11 @@
 // Heads beyond 128 channels: an item is one tile, whose products (2048 clocks) the softmax of half a tile at a time still overlaps: 9472 x 8192, 8
 // heads of 256 520 us, 1220 TFLOP/s (in tiles on the FP32 pipes 2000 x 3000 takes 1843 us, here 62); their keys are not divided.
 // CTAs are persistent, one per SM (contexts of one tile: two); the next item's Q, K and scores are under way during an item's last rows.
-// Rounded to bf16 are P (a half step, 2^-9 of a value, as the operand type asks) and the output; S, O, maxima and sums are fp32.
+// Rounded to bf16 are P (a half step, up to 2^-8 of a value, as the operand type asks) and the output; S, O, maxima and sums are fp32.
 // What bounds it.  A tile of 128 rows x 128 keys with heads of 128 takes the tensor core 1024 clocks (4096 multiply-adds each) and the special
 // function units as many (16 exponentials each): 9472 x 8192, 16 heads 477 us in a burst, 1330 TFLOP/s of the 1625 that a large matrix
 // product reaches, tensor pipe 62 % busy (4096 keys); run for long, the board's power holds back both (5400 x 14400 1060 TFLOP/s of 1397).
-// Heads of 64 halve the products and leave the exponentials: 8 x 1350 x 1350, 30 heads 192 us, special function units 63 % busy, the rest the
+// Heads of 64 halve the products and leave the exponentials: 8 x 1350 x 1350, 30 heads 187 us, special function units 63 % busy, the rest the
 // chain of scores, maximum, exponentials and product, which two tiles overlap and tensor memory has no room for a third.
 // Keys behind a row's length: scores are replaced before the maximum, P is zero there, and the up to 15 rows of V that the last
 // product still reads are zeroed in shared memory, since 0 * NaN is NaN.
