@@ -407,12 +407,15 @@ __device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
     asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
     return v;
 }
+// cc::wait_cluster with a limit of the call's
 __device__ __forceinline__ bool heard(const Params& a, uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
-    if (a.meeting_limit < 0) {
-        *abort_flag = 1;
-        return false;
-    }
-    return cc::wait_cluster(smem_u32(bar), parity, abort_flag, a.meeting_limit);
+    const long long t0 = clock64();
+    while (a.meeting_limit < 0 || !cc::try_wait_cluster(smem_u32(bar), parity))
+        if (a.meeting_limit < 0 || clock64() - t0 > a.meeting_limit) {
+            *abort_flag = 1;
+            return false;
+        }
+    return true;
 }
 // The CTAs of a cluster have each taken a share of an item's keys: they show one another half of the channels at a time, in fp32, and each
 // adds up (in the order of the shares) and writes its part of the tile's rows.  By the 128 threads of tile s; `rounds` counts what these
