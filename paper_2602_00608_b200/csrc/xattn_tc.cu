@@ -117,6 +117,8 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
+// of a wait within a CTA, which may be for a role or a tile that is at a meeting
+template <bool SPLIT> __device__ __forceinline__ long long limit(const Params& a) { return SPLIT ? a.wait_limit : WAIT_LIMIT_CYCLES; }
 // Scores become exponents by one fused multiply-add, score * scale - reference, whose product is not rounded while the reference is one
 // that was: half a step of the reference is left over, a common factor, which beyond 2^31 is an exponent of hundreds. So scores
 // beyond FAR are scaled by a power of two instead, which rounds nothing. They lie 32 or more apart there (a step of fp32), so nothing but the largest
@@ -162,7 +164,8 @@ __device__ __forceinline__ void hand_over(uint64_t* bar, int lane) {
 }
 // One row's tile of scores: exponentials into P.  Where P lies over the scores, 32 of them make 16 columns of it, so those still to be read
 // are not touched.
-template <int DP> struct Tile {
+template <int DP, bool SPLIT> struct Tile {
+    const Params& params;
     Scaled to_log2;
     uint32_t t_s, t_p, t_o;
     bool rescale;                // O holds something
@@ -226,7 +229,7 @@ template <int DP> struct Tile {
     // (Without a barrier to wait for: the scores were issued behind the last product into O and of P, which is complete then.)
     __device__ __forceinline__ void wait_pv() {
         if (!pv_done) return;
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(pv_done), pv_parity, abort_flag)) && ok;
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(pv_done), pv_parity, abort_flag, limit<SPLIT>(params))) && ok;
         tc_fence_after();
     }
     // All 128 keys count.  The maximum is only needed to see that the reference may stay, so it is taken half a tile at a time in front
@@ -604,10 +607,10 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
             unsigned long long sum = 0, sum_b = 0;           // of even and odd pairs of keys
             bool bad = false;
             for (int j = 0; j < it.n; ++j, ++n_s) {
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->s_full[s]), n_s & 1, abort_flag)) && ok;
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->s_full[s]), n_s & 1, abort_flag, limit<SPLIT>(a))) && ok;
                 tc_fence_after();
                 const int valid = it.len - (it.j0 + j) * KEYS;
-                Tile<DP> tile{{a.scale_log2, a.scale_far}, t_s, t_p, t_o, j > 0, C::APART && j + 1 < it.n ? &bars->s_free[s] : nullptr,
+                Tile<DP, SPLIT> tile{a, {a.scale_log2, a.scale_far}, t_s, t_p, t_o, j > 0, C::APART && j + 1 < it.n ? &bars->s_free[s] : nullptr,
                               C::APART && j > 0 ? &bars->pv_done[s] : nullptr, n_pv & 1, abort_flag, lane, m_ref, sum, sum_b};
                 if (C::APART && j > 0) ++n_pv;
                 float tmax;
@@ -621,7 +624,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
                 hand_over(&bars->p_part[s][1], lane);
             }
             if (it.n) {
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->o_full[s]), n_o & 1, abort_flag)) && ok;
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->o_full[s]), n_o & 1, abort_flag, limit<SPLIT>(a))) && ok;
                 tc_fence_after();
                 ++n_o;
             }
@@ -692,7 +695,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
                 if (!ok) break;
                 if (!it.n) continue;
                 const int buf = q_issued % C::Q_BUFS;
-                ok = mbar_wait(smem_u32(&bars->q_empty[buf]), ((q_issued / C::Q_BUFS) & 1) ^ 1, abort_flag, SPLIT ? a.wait_limit : WAIT_LIMIT_CYCLES);
+                ok = mbar_wait(smem_u32(&bars->q_empty[buf]), ((q_issued / C::Q_BUFS) & 1) ^ 1, abort_flag, limit<SPLIT>(a));
                 if (!ok) break;
                 const uint32_t qf = smem_u32(&bars->q_full[buf]);
                 mbar_arrive_expect_tx(qf, (uint32_t)(it.streams * C::CHUNKS * a.g * a.nt * 128));
@@ -701,7 +704,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
                         tma_load_5d(smem_u32(smem_q + (buf * 2 + s) * C::TILE_BYTES + c * (ROWS * 128)), &tm_q, c * CHUNK, 0, it.t0 + s * a.nt, it.kvh, it.b, qf);
                 ++q_issued;
                 for (int j = 0; j < 2 * it.n && ok; ++j) {
-                    ok = mbar_wait(smem_u32(&bars->empty[st]), ph ^ 1, abort_flag, SPLIT ? a.wait_limit : WAIT_LIMIT_CYCLES);
+                    ok = mbar_wait(smem_u32(&bars->empty[st]), ph ^ 1, abort_flag, limit<SPLIT>(a));
                     if (!ok) break;
                     const uint32_t full = smem_u32(&bars->full[st]);
                     mbar_arrive_expect_tx(full, C::TILE_BYTES);
@@ -719,7 +722,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
             }
             // Everything has landed once it has been multiplied; if a wait gave up anywhere, before the CTA's memory goes.
             for (int k = 0; k < C::STAGES && ok; ++k) {
-                ok = mbar_wait(smem_u32(&bars->empty[st]), ph ^ 1, abort_flag, SPLIT ? a.wait_limit : WAIT_LIMIT_CYCLES);
+                ok = mbar_wait(smem_u32(&bars->empty[st]), ph ^ 1, abort_flag, limit<SPLIT>(a));
                 if (ok && ++st == C::STAGES) { st = 0; ph ^= 1; }
             }
             if (!ok) {
@@ -740,7 +743,7 @@ xattn_tc_kernel(const __grid_constant__ Params a, const __grid_constant__ CUtens
         uint32_t st = 0, ph = 0, n_q = 0;
         auto wait_on = [&](uint64_t* bar, uint32_t parity) {
             const uint32_t p = smem_u32(bar);
-            if (!mbar_try_wait(p, parity)) (void)mbar_wait(p, parity, abort_flag, SPLIT ? a.wait_limit : WAIT_LIMIT_CYCLES);
+            if (!mbar_try_wait(p, parity)) (void)mbar_wait(p, parity, abort_flag, limit<SPLIT>(a));
             tc_fence_after();
         };
         auto commit = [&](uint64_t* bar) { umma_commit_on(smem_u32(bar), on); };
